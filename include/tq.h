@@ -354,6 +354,230 @@ tq_status tq_chain_sync_init(void* sync, const tq_chain_info* info, void* stream
  * one sync block must not overlap in time. */
 tq_status tq_gemv_chain(const void* plan, void* sync, const tq_chain_info* info, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The 4-bit side of a decode step: products with 4-bit weights (an output
+ * head, a projection kept at 4 bits) and a paged key/value cache held in 4
+ * bits with the attention that reads it.  All of it is added to ABI 7;
+ * nothing above changed.
+ *
+ * A value is offset + scale * code, code 0..15, with an fp16 scale and
+ * offset per group of 32, 64 or 128 values that lie next to each other.
+ * Quantising a group x of fp16 values (tq_q4_quantize, tq_kv_append), in
+ * fp32 with every operation rounded to nearest even:
+ *     offset = min x;  scale = fp16((max x - min x) / 15);
+ *     code   = clamp(rint((x - offset) / scale), 0, 15), 0 where scale is 0.
+ * A group that holds an infinity or a NaN gets NaN for scale and offset (its
+ * codes are 0), so that its values read back as NaN.
+ *
+ * Codes lie in 32-bit words of eight: the nibble 0, 4, 1, 5, 2, 6, 3, 7 of
+ * the word (nibble 0 the lowest four bits) holds element 0, 1, ..., 7.
+ */
+#define TQ_Q4_MAX_BATCH 64      /* rows of X in tq_q4_gemm */
+#define TQ_Q4_MAX_OUT (1 << 26)  /* outputs and inputs of a 4-bit matrix */
+#define TQ_Q4_MAX_IN (1 << 20)
+#define TQ_KV_MAX_ROWS 1024     /* rows of a call that changes the page table */
+#define TQ_KV_MAX_PAGES (1 << 20)   /* pages of one sequence */
+
+/* Non-owning view of a matrix of 4-bit weights.  N and K may be any sizes;
+ * the last tile of rows and the last 128 inputs are filled up with codes and
+ * parameters of 0 (written by tq_q4_quantize).
+ *   codes   words [ceil(N/16)][ceil(K/128)][c 4][row 16][j 4]: the word of
+ *           row 16 T + r holds inputs 128 B + 32 j + 8 c + (0..7)
+ *   params  fp16 (scale, offset) pairs [ceil(N/16)][128/group * ceil(K/128)]
+ *           [row 16] */
+typedef struct tq_q4_matrix {
+  int64_t n_out;            /* N, 1 .. TQ_Q4_MAX_OUT; at most 2^24 - 1 tiles in all */
+  int64_t n_in;             /* K, 1 .. TQ_Q4_MAX_IN */
+  int32_t group;            /* 32, 64 or 128 */
+  int32_t reserved;         /* must be 0 */
+  const uint8_t* codes;     /* 16-byte aligned, tq_q4_code_bytes */
+  const uint16_t* params;   /* 16-byte aligned, tq_q4_param_bytes */
+} tq_q4_matrix;
+
+/* Bytes of the two buffers of a matrix (host functions; 0 for sizes or
+ * groups that are not supported). */
+size_t tq_q4_code_bytes(int64_t n_out, int64_t n_in);
+size_t tq_q4_param_bytes(int64_t n_out, int64_t n_in, int32_t group);
+
+/* Quantise fp16 weights w [N][K] (rows ldw >= K elements apart) into the
+ * buffers of `m` (written through `codes` and `params`, which the caller
+ * owns).  A group of the last, shorter kind covers the inputs that are
+ * there. */
+tq_status tq_q4_quantize(const uint16_t* w, int64_t ldw, const tq_q4_matrix* m,
+                         uint8_t* codes, uint16_t* params, void* stream);
+
+/* Dense fp16 w [N][K] of a 4-bit matrix: offset + scale * code in fp32 (one
+ * rounding), then rounded to fp16.  w is 2-byte aligned. */
+tq_status tq_q4_unpack_fp16(const tq_q4_matrix* m, uint16_t* w, void* stream);
+
+/* Y = X W^T for B = 1..TQ_Q4_MAX_BATCH rows of fp16 activations.
+ *   X  fp16, rows ldx >= K elements apart; 2-byte aligned
+ *   Y  [B][N], fp16 (TQ_OUT_FP16) or fp32 (TQ_OUT_FP32); 4-byte aligned
+ * scale * sum(code * x) + offset * sum(x) per group, every product exact,
+ * sums in fp32; a row's result depends on the row and on which of 1..16,
+ * 17..32, 33..64 B lies in, not on the other rows.  Where that is not finite
+ * the output is the fp32 sum of x times the weights formed one by one, so an
+ * infinite input under a weight that is not 0 gives an infinity. */
+tq_status tq_q4_gemm(const tq_q4_matrix* m, const uint16_t* X, int64_t ldx,
+                     int32_t B, void* Y, int32_t flags, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Key/value cache held in 4 bits, in pages.
+ *
+ * A page holds page_size tokens of one layer, all key/value heads: per head
+ * page_size / 32 records of 32 tokens,
+ *     key codes    words [half 2][c 4][t 16][j D/32]: channels 32 j + 8 c +
+ *                  (0..7) of token 16 half + t
+ *     value codes  words [D/64][c 4][ch 16][jd 4]: channel 64 l + 16 jd + ch
+ *                  of tokens 4 c + i (nibble i) and 16 + 4 c + i (nibble
+ *                  4 + i)
+ *     key params   fp16 (scale, offset) [D/group][token 32]
+ *     value params likewise
+ * so that a wave's 16-byte loads of a record are the operands of its matrix
+ * instructions.  Sequences live in slots: `pages` names the pages of a slot
+ * in order (the same pages in every layer), `lens` the tokens it holds, and
+ * refs[p] how many slots name page p (0: free).  All of the table is device
+ * memory that the calls below read and write in stream order; no call waits
+ * for the device, and the caller never needs to read it.
+ *
+ * Calls that take rows work on n_rows slots, seqs[i] (device int32 [n_rows];
+ * NULL: slot i).  A slot outside the cache and a slot named twice in a call
+ * that changes the table (the first one counts) are left out and counted in
+ * *d_err (device int32, may be NULL), like every other request that a call
+ * below says it refuses.  Where a table names no page of the pool (-1), its
+ * tokens are neither written nor read.
+ */
+typedef struct tq_kv_cache {
+  int32_t n_layers;         /* 1 .. 65535 */
+  int32_t n_kv_heads;       /* 1 .. 1024 */
+  int32_t head_dim;         /* D: 64, 128 or 256 */
+  int32_t group;            /* 32, 64 or 128, at most D */
+  int32_t page_size;        /* tokens: 32, 64, 128, 256, 512 or 1024 */
+  int32_t n_seqs;           /* slots */
+  int32_t max_pages;        /* pages of a slot, 1 .. TQ_KV_MAX_PAGES */
+  int32_t reserved;         /* must be 0 */
+  int64_t n_pages;          /* pages of the pool, 1 .. 2^30 */
+  uint8_t* data;            /* [n_layers][n_pages][tq_kv_page_bytes]; 16-byte aligned */
+  int32_t* pages;           /* [n_seqs][max_pages], -1 where there is none */
+  int32_t* lens;            /* [n_seqs] */
+  int32_t* refs;            /* [n_pages] */
+} tq_kv_cache;
+
+/* Rows of fp16 vectors: element d of head h of token t at
+ * data[t * token_stride + h * head_stride + d]; 2-byte aligned. */
+typedef struct tq_kv_rows {
+  const uint16_t* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} tq_kv_rows;
+
+/* Bytes of one page of one layer (host function; 0 for a cache whose sizes
+ * are not supported). */
+size_t tq_kv_page_bytes(const tq_kv_cache* cache);
+
+/* Room for new tokens.  Row i gets cu_new[i+1] - cu_new[i] tokens (device
+ * int32 [n_rows + 1]; NULL: one each): the pages it lacks are taken from the
+ * free ones, lowest first, rows in order, its length grows, and starts[i]
+ * (device int32 [n_rows]) becomes the length it had.  A row whose pages are
+ * not there (more than are free behind the rows before it, or than max_pages)
+ * and one whose last page is partly filled and shared keep their length, get
+ * starts[i] = -1 and count in *d_err; the pages such a row asked for are not
+ * given to later rows of the call. */
+tq_status tq_kv_extend(const tq_kv_cache* cache, const int32_t* seqs, const int32_t* cu_new,
+                       int32_t n_rows, int32_t* starts, int32_t* d_err, void* stream);
+
+/* Give back every page of the rows' slots (a page is free once no slot
+ * names it) and empty them. */
+tq_status tq_kv_free(const tq_kv_cache* cache, const int32_t* seqs, int32_t n_rows,
+                     int32_t* d_err, void* stream);
+
+/* Bytes of workspace for tq_kv_fork of n_rows rows and for tq_kv_compact
+ * (n_rows = 0). */
+size_t tq_kv_workspace_bytes(const tq_kv_cache* cache, int32_t n_rows);
+
+/* Slots children[i] become copies of slots parents[i], as those are before
+ * the call: full pages are shared, a last page that is partly filled is
+ * copied (all layers) into a page of its own, lowest free page first, rows in
+ * order.  Refused: a child that holds tokens, is its own parent or comes
+ * twice, and a child whose page is not there.  Workspace: 16-byte aligned. */
+tq_status tq_kv_fork(const tq_kv_cache* cache, const int32_t* parents, const int32_t* children,
+                     int32_t n_rows, int32_t* d_err, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* Move pages so that the n pages in use become pages 0 .. n-1: the k-th page
+ * in use at or above n moves, in all layers, into the k-th free page below
+ * n, and the table and the counts follow.  n_live (device int32 [1], may be
+ * NULL) gets n; every byte of data behind page n-1 of a layer is free then.
+ * Workspace: 16-byte aligned. */
+tq_status tq_kv_compact(const tq_kv_cache* cache, int32_t* n_live, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* Copy whole pages src[i] -> dst[i] (device int32 [n], n <= 65535) in all layers; the
+ * table stays as it is.  No page may be a destination twice, or a source
+ * and a destination.  Pairs with a page outside the pool are refused. */
+tq_status tq_kv_copy_pages(const tq_kv_cache* cache, const int32_t* src, const int32_t* dst,
+                           int32_t n, int32_t* d_err, void* stream);
+
+/* Quantise new keys and values of one layer into the cache.  Row i's tokens
+ * are cu_new[i] .. cu_new[i+1]-1 of k and v (NULL: token i; at most max_new
+ * a row, n_tokens in all) and go to positions starts[i], starts[i] + 1, ...
+ * of its slot; a row with starts[i] < 0 is left out.  n_rows <= 65535,
+ * max_new <= 2^26.  Tokens past max_new,
+ * past n_tokens or without a page are left out and the row counts in *d_err
+ * (once).  Two rows of a call may not write the same record. */
+tq_status tq_kv_append(const tq_kv_cache* cache, int32_t layer, const int32_t* seqs,
+                       const int32_t* starts, const int32_t* cu_new, int32_t n_rows,
+                       int32_t n_tokens, int32_t max_new, const tq_kv_rows* k,
+                       const tq_kv_rows* v, int32_t* d_err, void* stream);
+
+/* The values of cached tokens as fp16 k_out, v_out [n_tokens][n_kv_heads][D]
+ * (offset + scale * code in fp32, rounded to fp16; 16-byte aligned), rows and
+ * positions as in tq_kv_append.  What has no page, and every token of a row
+ * with starts[i] < 0, reads as 0. */
+tq_status tq_kv_read(const tq_kv_cache* cache, int32_t layer, const int32_t* seqs,
+                     const int32_t* starts, const int32_t* cu_new, int32_t n_rows,
+                     int32_t n_tokens, int32_t max_new, uint16_t* k_out, uint16_t* v_out,
+                     void* stream);
+
+/* Attention of n_rows rows over their slots' pages of one layer.  Row i's
+ * queries are tokens cu_q[i] .. cu_q[i+1]-1 of q (NULL: token i, one a row),
+ * the last tokens of its slot: query t of n sits at position p = lens - n +
+ * t and attends to the positions j <= p, and j > p - window where window > 0.
+ * Query head h reads key/value head h / (n_heads / n_kv_heads).
+ *     o = sum_j softmax_j(scale * q . k_j) v_j;   lse = log sum_j exp(scale * q . k_j)
+ * A query with nothing to attend to gives o = 0 and lse = -infinity.
+ * Positions whose page the table does not name are left out.  Tokens past
+ * max_q of a row and past n_tokens are not computed.
+ *   max_len  the longest length among the slots, as far as the caller knows
+ *            (0: max_pages * page_size).  It decides how the work is split,
+ *            not what is read: longer slots are right, and slower.
+ *   o        [n_tokens][n_heads][D], fp16 or fp32 per flags; 16-byte aligned
+ *   lse      fp32 [n_tokens][n_heads], may be NULL
+ * Products are exact, the softmax, its sums and o's are fp32; a probability
+ * enters the matrix instructions as two fp16 numbers, 22 bits of it.
+ * The workspace (16-byte aligned) holds what parts of a long cache give:
+ * tq_kv_attention_workspace_bytes of the same arguments, which may be 0. */
+typedef struct tq_kv_attn {
+  int32_t n_rows;           /* >= 1 */
+  int32_t n_tokens;         /* tokens of q and o, >= 1 */
+  int32_t max_q;            /* queries of a row, >= 1 */
+  int32_t n_heads;          /* a multiple of n_kv_heads */
+  int32_t max_len;
+  int32_t window;           /* 0: none */
+  float scale;
+  int32_t flags;            /* TQ_OUT_FP16 or TQ_OUT_FP32 */
+  const int32_t* seqs;
+  const int32_t* cu_q;
+  tq_kv_rows q;
+  void* o;
+  float* lse;
+  void* workspace;
+  size_t workspace_bytes;
+} tq_kv_attn;
+
+size_t tq_kv_attention_workspace_bytes(const tq_kv_cache* cache, const tq_kv_attn* a);
+tq_status tq_kv_attention(const tq_kv_cache* cache, int32_t layer, const tq_kv_attn* a, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,6 +17,8 @@ What it computes (paper: section 3, eq. 3; section 12):
 * ``quantize``   — E2M-ATQ group ternarisation (section 4.2, eqs. 4-6): the
                    offset, thresholded supports, least-squares scales and
                    their refinement, and the choice of two-plane groups.
+* ``q4``         — the 4-bit operators: quantiser, layouts, product, attention
+                   over cached tokens, and the page table row by row.
 
 Parity status: codec, packed, accounting and quantize are pinned by tests in
 ``tests/test_oracle_*.py`` (brute force over all codes, exact rational
@@ -25,4 +27,4 @@ least-squares solver, and the paper's printed bit-accounting figures).  The pape
 so agreement with *the paper's own numbers* is pinned only for accounting.
 """
 
-from . import accounting, codec, packed, quantize  # noqa: F401
+from . import accounting, codec, packed, q4, quantize  # noqa: F401

@@ -1,0 +1,145 @@
+// What the 4-bit operators share: their device-side views, launchers and the
+// words of eight codes.  Every launcher assumes its arguments were checked
+// on the host (q4_api.hip) and returns the status of the launch.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/tq.h"
+
+namespace tq {
+
+// ---- Matrices (q4.hip).
+struct Q4Dev {
+  const uint8_t* codes;
+  const uint16_t* params;
+  int32_t n_out, n_in, group;
+};
+
+hipError_t launch_q4_quantize(const uint16_t* w, int64_t ldw, const Q4Dev& m, uint8_t* codes, uint16_t* params,
+                              hipStream_t s);
+hipError_t launch_q4_unpack(const Q4Dev& m, uint16_t* w, hipStream_t s);
+hipError_t launch_q4_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s);
+
+// ---- Cache (kvcache.hip, kvpages.hip, kvattn.hip).
+__host__ __device__ inline int64_t kv_record_bytes(int D, int G) { return 32 * (int64_t)(D + 8 * D / G); }
+
+struct KvDev {
+  uint8_t* data;
+  int32_t* pages;
+  int32_t* lens;
+  int32_t* refs;
+  int64_t page_bytes;
+  int64_t layer_bytes;   // n_pages * page_bytes
+  int32_t n_layers, H, D, G, page_size, page_shift, n_seqs, max_pages, n_pages;
+};
+
+struct KvRows {
+  const uint16_t* p;
+  int64_t ts, hs;
+};
+
+hipError_t launch_kv_append(const KvDev& c, int layer, const int32_t* seqs, const int32_t* starts,
+                            const int32_t* cu, int n_rows, int n_tokens, int max_new, const KvRows& k,
+                            const KvRows& v, int32_t* d_err, hipStream_t s);
+hipError_t launch_kv_read(const KvDev& c, int layer, const int32_t* seqs, const int32_t* starts, const int32_t* cu,
+                          int n_rows, int n_tokens, int max_new, uint16_t* k, uint16_t* v, hipStream_t s);
+
+hipError_t launch_kv_extend(const KvDev& c, const int32_t* seqs, const int32_t* cu, int n_rows, int32_t* starts,
+                            int32_t* d_err, hipStream_t s);
+hipError_t launch_kv_free(const KvDev& c, const int32_t* seqs, int n_rows, int32_t* d_err, hipStream_t s);
+size_t kv_workspace_bytes(const KvDev& c, int n_rows);
+hipError_t launch_kv_fork(const KvDev& c, const int32_t* parents, const int32_t* children, int n_rows,
+                          int32_t* d_err, void* ws, hipStream_t s);
+hipError_t launch_kv_compact(const KvDev& c, int32_t* n_live, void* ws, hipStream_t s);
+hipError_t launch_kv_copy_pages(const KvDev& c, const int32_t* src, const int32_t* dst, int n, int32_t* d_err,
+                                hipStream_t s);
+
+struct AttnCall {
+  int32_t n_rows, n_tokens, max_q, n_heads, max_len, window;
+  float scale;
+  bool out_f32;
+  const int32_t* seqs;
+  const int32_t* cu;
+  KvRows q;
+  void* o;
+  float* lse;
+  void* ws;
+};
+// false where the launch would not fit a grid.
+bool kv_attention_plan(const KvDev& c, const AttnCall& a, size_t* ws_bytes);
+hipError_t launch_kv_attention(const KvDev& c, int layer, const AttnCall& a, hipStream_t s);
+
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+
+// Eight fp16 values from anywhere (2-byte aligned): one 16-byte load, which
+// the hardware takes at any address.
+struct __attribute__((packed, aligned(2))) half8_u {
+  half8 v;
+};
+__device__ inline half8 load8(const uint16_t* p) { return reinterpret_cast<const half8_u*>(p)->v; }
+
+// A word of eight codes as an operand of a matrix instruction: code n as the
+// fp16 number n - 8, register r the nibbles r and r + 4.  The bits of a code
+// go under those of 1024 (or, 4 bits up, of 64), which makes it 1024 + n (64 +
+// n), and the subtraction is exact.  Around 0, because a sum of codes and the
+// sum that its offset multiplies cancel where the values do: with offset +
+// 8 scale in the place of the offset both are small.  (The codes' bits as
+// they are, subnormal numbers, would save the additions; the matrix cores
+// align such operands by their exponent alone and lose 7 bits of the sum:
+// 1.6e-3 off at 131072 tokens where this is below 2e-6.)
+__device__ inline half8 code_operand(uint32_t w) {
+  const half2v a = {(_Float16)-1032.0f, (_Float16)-1032.0f}, b = {(_Float16)-72.0f, (_Float16)-72.0f};
+  const uint32_t t = w >> 8;
+  const half2v r0 = __builtin_bit_cast(half2v, (w & 0x000F000Fu) | 0x64006400u) + a;
+  const half2v r1 = __builtin_bit_cast(half2v, (w & 0x00F000F0u) | 0x54005400u) + b;
+  const half2v r2 = __builtin_bit_cast(half2v, (t & 0x000F000Fu) | 0x64006400u) + a;
+  const half2v r3 = __builtin_bit_cast(half2v, (t & 0x00F000F0u) | 0x54005400u) + b;
+  return half8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
+}
+// The offset that goes with codes around 0.
+__device__ inline float centred(float s, float m) { return fmaf(8.0f, s, m); }
+
+// Nibble of element e of eight, and eight codes as a word.
+__device__ inline constexpr int nibble_of(int e) { return (e & 1) * 4 + (e >> 1); }
+__device__ inline uint32_t code_word(const uint32_t* q) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w |= q[e] << (4 * nibble_of(e));
+  return w;
+}
+
+// The quantiser's arithmetic for one group: scale and offset from the
+// smallest and largest value, and a code.
+struct Q4Params {
+  _Float16 s, m;
+};
+__device__ inline Q4Params q4_params(float lo, float hi, bool finite) {
+  Q4Params p;
+  p.m = (_Float16)lo;
+  p.s = (_Float16)__fdiv_rn(__fsub_rn(hi, lo), 15.0f);
+  if (!finite) p.s = p.m = (_Float16)__builtin_nanf("");
+  return p;
+}
+__device__ inline uint32_t q4_code(float x, float lo, float s) {
+  // s is 0, positive or NaN
+  if (!(s > 0.0f)) return 0;
+  const float q = rintf(__fdiv_rn(__fsub_rn(x, lo), s));
+  return (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f);
+}
+__device__ inline float q4_value(uint32_t q, float s, float m) { return fmaf((float)q, s, m); }
+
+__device__ inline uint32_t pair_bits(Q4Params p) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, p.s) | ((uint32_t)__builtin_bit_cast(uint16_t, p.m) << 16);
+}
+__device__ inline float lo_half(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
+__device__ inline float hi_half(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(b >> 16)); }
+
+}  // namespace tq

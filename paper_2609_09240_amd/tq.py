@@ -23,6 +23,8 @@ OUT_FP16 = 0
 OUT_FP32 = 1
 MAX_GROUPED = 8
 MAX_BATCH = 64
+Q4_MAX_BATCH = 64
+KV_MAX_ROWS = 1024
 
 STATUS = {0: "TQ_OK", 1: "TQ_ERR_NULL", 2: "TQ_ERR_SHAPE", 3: "TQ_ERR_ALIGN",
           4: "TQ_ERR_UNSUPPORTED", 5: "TQ_ERR_HIP"}
@@ -74,6 +76,63 @@ class TqChainInfo(ctypes.Structure):
     ]
 
 
+class TqQ4Matrix(ctypes.Structure):
+    _fields_ = [
+        ("n_out", ctypes.c_int64),
+        ("n_in", ctypes.c_int64),
+        ("group", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("codes", ctypes.c_void_p),
+        ("params", ctypes.c_void_p),
+    ]
+
+
+class TqKvCache(ctypes.Structure):
+    _fields_ = [
+        ("n_layers", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("group", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("n_pages", ctypes.c_int64),
+        ("data", ctypes.c_void_p),
+        ("pages", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p),
+        ("refs", ctypes.c_void_p),
+    ]
+
+
+class TqKvRows(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+    ]
+
+
+class TqKvAttn(ctypes.Structure):
+    _fields_ = [
+        ("n_rows", ctypes.c_int32),
+        ("n_tokens", ctypes.c_int32),
+        ("max_q", ctypes.c_int32),
+        ("n_heads", ctypes.c_int32),
+        ("max_len", ctypes.c_int32),
+        ("window", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("flags", ctypes.c_int32),
+        ("seqs", ctypes.c_void_p),
+        ("cu_q", ctypes.c_void_p),
+        ("q", TqKvRows),
+        ("o", ctypes.c_void_p),
+        ("lse", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -86,6 +145,7 @@ def lib():
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         mp = ctypes.POINTER(TqMatrix)
+        qp, cp, rp = ctypes.POINTER(TqQ4Matrix), ctypes.POINTER(TqKvCache), ctypes.POINTER(TqKvRows)
         sigs = {
             "tq_abi_version": ([], ctypes.c_int),
             "tq_status_string": ([ctypes.c_int], ctypes.c_char_p),
@@ -104,6 +164,22 @@ def lib():
                               ctypes.c_int),
             "tq_chain_sync_init": ([vp, ctypes.POINTER(TqChainInfo), vp], ctypes.c_int),
             "tq_gemv_chain": ([vp, vp, ctypes.POINTER(TqChainInfo), vp], ctypes.c_int),
+            "tq_q4_code_bytes": ([i64, i64], ctypes.c_size_t),
+            "tq_q4_param_bytes": ([i64, i64, i32], ctypes.c_size_t),
+            "tq_q4_quantize": ([vp, i64, qp, vp, vp, vp], ctypes.c_int),
+            "tq_q4_unpack_fp16": ([qp, vp, vp], ctypes.c_int),
+            "tq_q4_gemm": ([qp, vp, i64, i32, vp, i32, vp], ctypes.c_int),
+            "tq_kv_page_bytes": ([cp], ctypes.c_size_t),
+            "tq_kv_extend": ([cp, vp, vp, i32, vp, vp, vp], ctypes.c_int),
+            "tq_kv_free": ([cp, vp, i32, vp, vp], ctypes.c_int),
+            "tq_kv_workspace_bytes": ([cp, i32], ctypes.c_size_t),
+            "tq_kv_fork": ([cp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
+            "tq_kv_compact": ([cp, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
+            "tq_kv_copy_pages": ([cp, vp, vp, i32, vp, vp], ctypes.c_int),
+            "tq_kv_append": ([cp, i32, vp, vp, vp, i32, i32, i32, rp, rp, vp, vp], ctypes.c_int),
+            "tq_kv_read": ([cp, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp], ctypes.c_int),
+            "tq_kv_attention_workspace_bytes": ([cp, ctypes.POINTER(TqKvAttn)], ctypes.c_size_t),
+            "tq_kv_attention": ([cp, i32, ctypes.POINTER(TqKvAttn), vp], ctypes.c_int),
         }
         for name, (args, res) in sigs.items():
             fn = getattr(L, name)
@@ -484,3 +560,295 @@ def quantize_linear(W, f2=0.1, iters=4, host_rowptr=True, group_offsets=False, s
     if group_offsets:
         kw["offset0"] = mu0.reshape(N, ng)
     return PackedLinear(N, K, codes0, s0.reshape(N, ng), **kw)
+
+
+# --------------------------------------------------------------------------
+# Products with 4-bit weights.
+# --------------------------------------------------------------------------
+
+class Q4Linear:
+    """A matrix of 4-bit weights in device memory (the buffers tq_q4_matrix
+    points at): codes uint8, params float16, both flat and in the library's
+    layout.  The buffers are fixed when it is made; their contents may
+    change."""
+
+    __slots__ = ("n_out", "n_in", "group", "codes", "params", "_ref")
+
+    def __init__(self, n_out, n_in, group, codes, params):
+        _cuda(codes, torch.uint8, "codes")
+        _cuda(params, torch.float16, "params")
+        nc, np_ = lib().tq_q4_code_bytes(n_out, n_in), lib().tq_q4_param_bytes(n_out, n_in, group)
+        if nc == 0 or np_ == 0:
+            raise TqError(4, "Q4Linear")
+        if codes.numel() != nc or 2 * params.numel() != np_:
+            raise ValueError(f"codes and params must hold {nc} and {np_} bytes")
+        self.n_out, self.n_in, self.group, self.codes, self.params = n_out, n_in, group, codes, params
+        self._ref = ctypes.pointer(TqQ4Matrix(n_out, n_in, group, 0, codes.data_ptr(), params.data_ptr()))
+
+    @classmethod
+    def empty(cls, n_out, n_in, group=GROUP, device="cuda"):
+        """Buffers for a matrix, not yet written."""
+        nc, np_ = lib().tq_q4_code_bytes(n_out, n_in), lib().tq_q4_param_bytes(n_out, n_in, group)
+        return cls(n_out, n_in, group, torch.empty(nc, dtype=torch.uint8, device=device),
+                   torch.empty(np_ // 2, dtype=torch.float16, device=device))
+
+    def nbytes(self):
+        return self.codes.numel() + 2 * self.params.numel()
+
+
+def _fp16_rows(t, name):
+    """fp16 [rows, K] on the GPU with adjacent elements; any row stride."""
+    if not (t.is_cuda and t.dtype == torch.float16 and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
+        raise ValueError(f"{name} must be a float16 matrix on the GPU with adjacent elements in a row")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def tq_q4_quantize(w, group=GROUP, mat=None, stream=None):
+    """Q4Linear of dense fp16 weights w [N, K]."""
+    ldw = _fp16_rows(w, "w")
+    if mat is None:
+        mat = Q4Linear.empty(w.shape[0], w.shape[1], group, w.device)
+    elif (mat.n_out, mat.n_in) != tuple(w.shape):
+        raise ValueError("w does not have the shape of mat")
+    _check(lib().tq_q4_quantize(_ptr(w), ldw, mat._ref, _ptr(mat.codes), _ptr(mat.params), _stream(stream)),
+           "tq_q4_quantize")
+    _used_on(stream, w, mat.codes, mat.params)
+    return mat
+
+
+def tq_q4_unpack_fp16(mat, w=None, stream=None):
+    """Dense fp16 [N, K] of a Q4Linear."""
+    if w is None:
+        w = torch.empty((mat.n_out, mat.n_in), dtype=torch.float16, device=mat.codes.device)
+    _out_buffer(w, (mat.n_out, mat.n_in), torch.float16, "w")
+    _check(lib().tq_q4_unpack_fp16(mat._ref, _ptr(w), _stream(stream)), "tq_q4_unpack_fp16")
+    _used_on(stream, w, mat.codes, mat.params)
+    return w
+
+
+def _out_buffer(t, shape, dtype, name):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}")
+    _cuda(t, dtype, name)
+
+
+def tq_q4_gemm(mat, X, Y=None, out_f32=False, stream=None):
+    """Y = X W^T for fp16 X [B, K] (or x [K]), B up to Q4_MAX_BATCH; Y [B, N]
+    (or [N])."""
+    one = X.dim() == 1
+    if one:
+        X = X.unsqueeze(0)
+    ldx = _fp16_rows(X, "X")
+    B = X.shape[0]
+    if X.shape[1] != mat.n_in:
+        raise ValueError(f"X must have {mat.n_in} columns")
+    dtype = torch.float32 if out_f32 else torch.float16
+    shape = (mat.n_out,) if one else (B, mat.n_out)
+    if Y is None:
+        Y = torch.empty(shape, dtype=dtype, device=X.device)
+    else:
+        _out_buffer(Y, shape, dtype, "Y")
+    _check(lib().tq_q4_gemm(mat._ref, X.data_ptr(), ldx, B, Y.data_ptr(), OUT_FP32 if out_f32 else OUT_FP16,
+                            _stream(stream)), "tq_q4_gemm")
+    _used_on(stream, X, Y, mat.codes, mat.params)
+    return Y
+
+
+# --------------------------------------------------------------------------
+# The key/value cache held in 4 bits.
+# --------------------------------------------------------------------------
+
+class KVCache:
+    """A paged 4-bit key/value cache in device memory (the buffers tq_kv_cache
+    points at): data uint8 [n_layers, n_pages, page_bytes], pages int32
+    [n_seqs, max_pages] (-1: none), lens int32 [n_seqs], refs int32 [n_pages].
+    The buffers are fixed when it is made; their contents belong to the
+    calls below.  One cache serves one stream at a time: calls on another
+    one are the caller's to order."""
+
+    __slots__ = ("data", "pages", "lens", "refs", "n_kv_heads", "head_dim", "page_size", "group", "_c", "_ref")
+
+    def __init__(self, data, pages, lens, refs, n_kv_heads, head_dim, page_size=64, group=64):
+        _cuda(data, torch.uint8, "data")
+        for t, name in ((pages, "pages"), (lens, "lens"), (refs, "refs")):
+            _cuda(t, torch.int32, name)
+        if data.dim() != 3 or pages.dim() != 2 or lens.shape != pages.shape[:1] or refs.shape != data.shape[1:2]:
+            raise ValueError("data [layers, n_pages, page_bytes], pages [n_seqs, max_pages], lens [n_seqs] and "
+                             "refs [n_pages] do not fit each other")
+        c = TqKvCache(data.shape[0], n_kv_heads, head_dim, group, page_size, pages.shape[0], pages.shape[1], 0,
+                      data.shape[1], data.data_ptr(), pages.data_ptr(), lens.data_ptr(), refs.data_ptr())
+        ref = ctypes.pointer(c)
+        want = lib().tq_kv_page_bytes(ref)
+        if want == 0:
+            raise TqError(4, "KVCache")
+        if data.shape[2] != want:
+            raise ValueError(f"a page has {want} bytes")
+        self.data, self.pages, self.lens, self.refs = data, pages, lens, refs
+        self.n_kv_heads, self.head_dim, self.page_size, self.group = n_kv_heads, head_dim, page_size, group
+        self._c, self._ref = c, ref
+
+    @classmethod
+    def empty(cls, n_layers, n_pages, n_seqs, max_pages, n_kv_heads, head_dim, page_size=64, group=64,
+              device="cuda"):
+        """A cache with every slot empty and every page free."""
+        c = TqKvCache(n_layers, n_kv_heads, head_dim, group, page_size, n_seqs, max_pages, 0, n_pages)
+        pb = lib().tq_kv_page_bytes(ctypes.byref(c))
+        if pb == 0:
+            raise TqError(4, "KVCache")
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.empty((n_layers, n_pages, pb), dtype=torch.uint8, device=device),
+                   torch.full((n_seqs, max_pages), -1, **i32), torch.zeros(n_seqs, **i32), torch.zeros(n_pages, **i32),
+                   n_kv_heads, head_dim, page_size, group)
+
+    def _buffers(self):
+        return self.data, self.pages, self.lens, self.refs
+
+
+def _i32(t, n, name):
+    """An int32 vector of n elements on the GPU, or None."""
+    if t is None:
+        return None
+    if t.dim() != 1 or t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements")
+    _cuda(t, torch.int32, name)
+    return t.data_ptr()
+
+
+def _n_rows(cache, seqs, cu):
+    if seqs is not None:
+        return seqs.numel()
+    return cu.numel() - 1 if cu is not None else cache.lens.numel()
+
+
+def tq_kv_extend(cache, cu_new=None, seqs=None, starts=None, d_err=None, stream=None):
+    """Room for new tokens: row i (slot seqs[i], or slot i) gets
+    cu_new[i + 1] - cu_new[i] of them (one without cu_new).  Returns starts,
+    the lengths before, -1 for a row that got none."""
+    n = _n_rows(cache, seqs, cu_new)
+    if starts is None:
+        starts = torch.empty(n, dtype=torch.int32, device=cache.lens.device)
+    _check(lib().tq_kv_extend(cache._ref, _i32(seqs, n, "seqs"), _i32(cu_new, n + 1, "cu_new"), n,
+                              _i32(starts, n, "starts"), _i32(d_err, 1, "d_err"), _stream(stream)), "tq_kv_extend")
+    _used_on(stream, seqs, cu_new, starts, d_err, *cache._buffers())
+    return starts
+
+
+def tq_kv_free(cache, seqs=None, d_err=None, stream=None):
+    """Empty the slots seqs (every slot without)."""
+    n = _n_rows(cache, seqs, None)
+    _check(lib().tq_kv_free(cache._ref, _i32(seqs, n, "seqs"), n, _i32(d_err, 1, "d_err"), _stream(stream)),
+           "tq_kv_free")
+    _used_on(stream, seqs, d_err, *cache._buffers())
+
+
+def _workspace(workspace, need, device):
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    _cuda(workspace, torch.uint8, "workspace")
+    return workspace
+
+
+def tq_kv_workspace_bytes(cache, n_rows=0):
+    """Workspace of tq_kv_fork of n_rows rows, or of tq_kv_compact."""
+    return int(lib().tq_kv_workspace_bytes(cache._ref, n_rows))
+
+
+def tq_kv_fork(cache, parents, children, d_err=None, workspace=None, stream=None):
+    """Empty slots children[i] become copies of slots parents[i]."""
+    n = parents.numel()
+    workspace = _workspace(workspace, tq_kv_workspace_bytes(cache, n), cache.lens.device)
+    _check(lib().tq_kv_fork(cache._ref, _i32(parents, n, "parents"), _i32(children, n, "children"), n,
+                            _i32(d_err, 1, "d_err"), workspace.data_ptr(), workspace.numel(), _stream(stream)),
+           "tq_kv_fork")
+    _used_on(stream, parents, children, d_err, workspace, *cache._buffers())
+
+
+def tq_kv_compact(cache, n_live=None, workspace=None, stream=None):
+    """Move the pages in use to the front of the pool; n_live (int32 [1])
+    gets their number."""
+    workspace = _workspace(workspace, tq_kv_workspace_bytes(cache), cache.lens.device)
+    _check(lib().tq_kv_compact(cache._ref, _i32(n_live, 1, "n_live"), workspace.data_ptr(), workspace.numel(),
+                               _stream(stream)), "tq_kv_compact")
+    _used_on(stream, n_live, workspace, *cache._buffers())
+
+
+def tq_kv_copy_pages(cache, src, dst, d_err=None, stream=None):
+    """Copy pages src[i] -> dst[i] in all layers."""
+    n = src.numel()
+    _check(lib().tq_kv_copy_pages(cache._ref, _i32(src, n, "src"), _i32(dst, n, "dst"), n, _i32(d_err, 1, "d_err"),
+                                  _stream(stream)), "tq_kv_copy_pages")
+    _used_on(stream, src, dst, d_err, *cache._buffers())
+
+
+def _kv_rows(t, heads, d, name):
+    """fp16 [T, heads, D] on the GPU as tq_kv_rows, any strides but the last."""
+    if not (t.is_cuda and t.dtype == torch.float16 and t.dim() == 3 and t.shape[2] == d and t.stride(2) == 1):
+        raise ValueError(f"{name} must be float16 [tokens, heads, {d}] on the GPU with adjacent channels")
+    if heads is not None and t.shape[1] != heads:
+        raise ValueError(f"{name} must have {heads} heads")
+    return TqKvRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def tq_kv_append(cache, layer, k, v, starts, seqs=None, cu_new=None, max_new=1, d_err=None, stream=None):
+    """Quantise keys and values k, v [T, n_kv_heads, D] into the cache at the
+    positions that tq_kv_extend gave (starts); row i's tokens are cu_new[i] ..
+    cu_new[i + 1] - 1 (token i without cu_new), at most max_new a row."""
+    n = starts.numel()
+    if k.shape != v.shape:
+        raise ValueError("k and v must have the same shape")
+    kr = _kv_rows(k, cache.n_kv_heads, cache.head_dim, "k")
+    vr = _kv_rows(v, cache.n_kv_heads, cache.head_dim, "v")
+    _check(lib().tq_kv_append(cache._ref, layer, _i32(seqs, n, "seqs"), _i32(starts, n, "starts"),
+                              _i32(cu_new, n + 1, "cu_new"), n, k.shape[0], max_new, kr, vr,
+                              _i32(d_err, 1, "d_err"), _stream(stream)), "tq_kv_append")
+    _used_on(stream, k, v, starts, seqs, cu_new, d_err, *cache._buffers())
+
+
+def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=1, k=None, v=None, stream=None):
+    """fp16 keys and values [n_tokens, n_kv_heads, D] of cached tokens; rows
+    and positions as in tq_kv_append."""
+    n = starts.numel()
+    shape = (n_tokens, cache.n_kv_heads, cache.head_dim)
+    if k is None:
+        k = torch.empty(shape, dtype=torch.float16, device=cache.lens.device)
+    if v is None:
+        v = torch.empty(shape, dtype=torch.float16, device=cache.lens.device)
+    _out_buffer(k, shape, torch.float16, "k")
+    _out_buffer(v, shape, torch.float16, "v")
+    _check(lib().tq_kv_read(cache._ref, layer, _i32(seqs, n, "seqs"), _i32(starts, n, "starts"),
+                            _i32(cu_new, n + 1, "cu_new"), n, n_tokens, max_new, k.data_ptr(), v.data_ptr(),
+                            _stream(stream)), "tq_kv_read")
+    _used_on(stream, k, v, starts, seqs, cu_new, *cache._buffers())
+    return k, v
+
+
+def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=1, max_len=0, scale=None, window=0, o=None,
+                    lse=None, out_f32=False, want_lse=False, workspace=None, stream=None):
+    """Attention of q [T, n_heads, D], the last tokens of their slots, over the
+    cache: o [T, n_heads, D] (fp16 or fp32), and with want_lse also the log of
+    the softmax's sum, fp32 [T, n_heads].  scale: 1 / sqrt(D) without."""
+    T, n_heads, D = q.shape
+    n = seqs.numel() if seqs is not None else (cu_q.numel() - 1 if cu_q is not None else T)
+    if cu_q is None and n != T:
+        raise ValueError("without cu_q, q must have one token a row")
+    qr = _kv_rows(q, None, cache.head_dim, "q")
+    dtype = torch.float32 if out_f32 else torch.float16
+    if o is None:
+        o = torch.empty((T, n_heads, D), dtype=dtype, device=q.device)
+    else:
+        _out_buffer(o, (T, n_heads, D), dtype, "o")
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((T, n_heads), dtype=torch.float32, device=q.device)
+    else:
+        _out_buffer(lse, (T, n_heads), torch.float32, "lse")
+    a = TqKvAttn(n, T, max_q, n_heads, max_len, window, D ** -0.5 if scale is None else scale,
+                 OUT_FP32 if out_f32 else OUT_FP16, _i32(seqs, n, "seqs"), _i32(cu_q, n + 1, "cu_q"), qr,
+                 o.data_ptr(), None if lse is None else lse.data_ptr(), None, 0)
+    need = lib().tq_kv_attention_workspace_bytes(cache._ref, a)
+    if need:
+        workspace = _workspace(workspace, need, q.device)
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(lib().tq_kv_attention(cache._ref, layer, a, _stream(stream)), "tq_kv_attention")
+    _used_on(stream, q, seqs, cu_q, o, lse, workspace, *cache._buffers())
+    return (o, lse) if lse is not None else o
