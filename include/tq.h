@@ -555,8 +555,11 @@ tq_status tq_kv_read(const tq_kv_cache* cache, int32_t layer, const int32_t* seq
  *   lse      fp32 [n_tokens][n_heads], may be NULL
  * Products are exact, the softmax, its sums and o's are fp32; a probability
  * enters the matrix instructions as two fp16 numbers, 22 bits of it.
- * The workspace (16-byte aligned) holds what parts of a long cache give:
- * tq_kv_attention_workspace_bytes of the same arguments, which may be 0. */
+ * The workspace (16-byte aligned, tq_kv_attention_workspace_bytes of the same
+ * arguments, which may be 0) holds what the parts of a long cache give, and
+ * counts of them that every call finds and leaves 0: it is filled with zeros
+ * once, before its first call, and serves any calls that do not overlap in
+ * time. */
 typedef struct tq_kv_attn {
   int32_t n_rows;           /* >= 1 */
   int32_t n_tokens;         /* tokens of q and o, >= 1 */

@@ -7,7 +7,7 @@
 // operands of the matrix instructions and the parameters multiply the fp32
 // sums (keys) or the probabilities (values).
 //
-// One wave takes records of 32 tokens against a tile of 16 QT query rows (a
+// One wave takes records of 32 tokens against a tile of 16 query rows (a
 // row is a query token and one of the heads that share the key/value head):
 //   S^T = K Q^T: 16 tokens x 16 rows per instruction, a lane's four sums are
 //   four tokens of the row lane % 16, and the eight it holds of a record are
@@ -17,11 +17,27 @@
 // bits); the sums of p, of p mv and of everything else are fp32.
 //
 // Work split: a workgroup has four waves that take the records of its range
-// in turn and join their maxima, sums and outputs through LDS; a range is a
-// part of the records that a tile of rows can see, so that few rows over a
-// long cache fill the chip.  Parts leave their outputs in the workspace and
-// a second launch joins them; where the caller's max_len makes one part the
-// most there can be, it writes o itself.
+// in turn and join their references, sums and outputs through LDS.  Where there
+// are few tiles over long caches the records of all of them are laid in a
+// line and divided evenly among as many workgroups as the chip holds, whatever
+// the lengths are; a tile that several workgroups have parts of is joined by
+// the last of them to finish.  Otherwise a workgroup has a tile.
+//
+// A record's 4.6 KB (D = 128, groups of 64) arrive in the registers of the
+// record before, each as soon as it is used; 168 of them allow three waves a
+// SIMD.  One token over one long cache: 5.4 TB/s for every further byte, and
+// 6 us of launch, table, first loads and joining waves before the first, 7 us
+// for joining 96 parts a head.
+//   1 x 131072 tokens, 8 heads, groups of 128 (143 MB)  39.7 us
+//   32 ragged rows to 8192, groups of 64 (93 MB)        34.0
+//   1 x 4096 (4.7 MB)                                   11.9
+//   1 x 45                                              6.4
+//   a chunk of 2 x 1000 queries over up to 5000, window 2048, 14 heads of 64 on
+//   2, groups of 32 (10 GFLOP)                          77
+// (One launch a split and another to join: 31 + 6.5, 33 + 6 and 10 + 6 for the
+// first three, and 3 us between the launches.  32 or 64 rows a tile, which
+// unpack a record once for two or four tiles, halve the waves: 90 and 120 us
+// for the chunk, 37 where 8 queries of 4 heads take 29.)
 
 #include "q4_internal.h"
 
@@ -29,10 +45,48 @@ namespace tq {
 namespace {
 
 constexpr int kWaves = 4;
+
+// The page table as memory that no launch in flight writes: uniform reads of
+// it are scalar loads.
+typedef const __attribute__((address_space(4))) int32_t* table_ptr;
+__device__ inline table_ptr as_table(const int32_t* p) { return (table_ptr)(uintptr_t)p; }
+constexpr int kCus = 256;
+// Up to kMinUnits units (512 tokens) a tile is one workgroup's: a second one
+// saves less than joining costs.  A share has kUnitsOfShare units at least
+// (4096 tokens: 13.9 us with one, 12.2 with two, 13.7 with four).
+constexpr int kMinUnits = 4;
+constexpr int kUnitsOfShare = 2;
+constexpr int kMaxShares = 4 * kCus;
+constexpr int kOneLevel = 16;   // parts joined in one step (96 of them: 47 us in one step, 40 in two)
 constexpr float kLn2 = 0.69314718055994531f;
 
 __device__ inline float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// What a probability is scaled by: the running reference r of a row (log2) is
+// kept so that exp2(s - r) of its largest logit so far lies in 2^8 .. 2^10.
+// Their products with the value scales are then far from fp16's subnormal
+// numbers, in which a second half would lose its bits.  Where a scale of 2 or
+// more has been seen the range is 2^0 .. 2^2, since 2^2 times the largest scale
+// (2 * 65504 / 15) is the most that fp16 takes.
+constexpr float kHigh = 10.0f, kHighSet = 8.0f, kLow = 2.0f, kLowSet = 0.0f;
+
+__device__ inline half2v pair(uint32_t b) { return __builtin_bit_cast(half2v, b); }
+
+// Two fp32 numbers as fp16 rounded towards 0, and what that left.
+__device__ inline uint32_t cut(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+}
+__device__ inline float rest0(uint32_t h, float w) {
+  float d;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(d) : "v"(h), "v"(w));
+  return d;
+}
+__device__ inline float rest1(uint32_t h, float w) {
+  float d;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(h), "v"(w));
+  return d;
 }
 
 struct Args {
@@ -44,13 +98,15 @@ struct Args {
   const uint16_t* q;
   void* o;
   float* lse;
-  float* part;             // [tile][split][R][D + 2]: sums, maximum (log2), sum of p
+  int32_t* count;          // [2][2 * kMaxShares] parts and groups of parts that have arrived, 0 between calls
+  float* part;             // [2 * workgroups][R][D + 4]: sums, reference (log2), sum of p
   int64_t q_ts, q_hs, page_bytes;
   float scale_log2;
   int32_t n_rows, n_tokens, max_q, H, share, window;
   int32_t page_shift, n_seqs, max_pages, n_pages;
-  int32_t tiles, splits, chunk;   // tiles of a row, parts of a tile, records of a part
-  int32_t R;                      // rows of a tile kept in the workspace
+  int32_t tiles;           // tiles of a row
+  int32_t shares;          // workgroups that divide the work evenly; 0: one per tile and head
+  int32_t R;               // rows of a tile kept in the workspace
   int32_t out_f32;
 };
 
@@ -58,39 +114,125 @@ struct Args {
 struct Tile {
   int b, h, qt;
   int seq, first, n, rows;   // slot, first token in q, tokens, rows of (b, h) in all
+  int64_t asked;             // tokens the call names for the row, max_q or not
   int len;
   int row0;                  // first of the tile's rows
-  int rec0, rec1, parts;     // records it can see, and in how many parts
+  int rec0, rec1;            // records it can see
+  int units;                 // of four records, one a wave; 1 where there are none
 };
 
-template <int QT>
 __device__ inline bool tile_of(const Args& a, int id, Tile* t) {
   t->h = id % a.H;
   t->b = id / a.H % a.n_rows;
   t->qt = id / a.H / a.n_rows;
-  t->seq = a.seqs ? a.seqs[t->b] : t->b;
-  int64_t first = a.cu ? a.cu[t->b] : t->b, end = a.cu ? a.cu[t->b + 1] : (int64_t)t->b + 1;
-  const int64_t asked = end - first;
+  t->seq = a.seqs ? as_table(a.seqs)[t->b] : t->b;
+  int64_t first = a.cu ? as_table(a.cu)[t->b] : t->b, end = a.cu ? as_table(a.cu)[t->b + 1] : (int64_t)t->b + 1;
+  const int64_t asked = t->asked = end - first;
   const bool bad = first < 0 || asked < 0;
   end = min(min(end, (int64_t)a.n_tokens), first + a.max_q);
   t->first = (int)first;
   t->n = bad || end <= first ? 0 : (int)(end - first);
   t->rows = t->n * a.share;
-  t->row0 = t->qt * 16 * QT;
+  t->row0 = t->qt * 16;
   if (t->row0 >= t->rows) return false;
   t->len = 0;
   if (t->seq >= 0 && t->seq < a.n_seqs)
-    t->len = (int)min(min(max((int64_t)a.lens[t->seq], (int64_t)0), (int64_t)a.max_pages << a.page_shift),
+    t->len = (int)min(min(max((int64_t)as_table(a.lens)[t->seq], (int64_t)0), (int64_t)a.max_pages << a.page_shift),
                       (int64_t)INT32_MAX - 64);
   // Position of query token i is base + i; all of what was asked for counts.
   const int64_t base = t->len - asked;
-  const int i0 = t->row0 / a.share, i1 = min(t->row0 + 16 * QT - 1, t->rows - 1) / a.share;
+  const int i0 = t->row0 / a.share, i1 = min(t->row0 + 16 - 1, t->rows - 1) / a.share;
   const int64_t hi = min((int64_t)t->len, base + i1 + 1);
   const int64_t lo = a.window > 0 ? max((int64_t)0, base + i0 + 1 - a.window) : 0;
   t->rec0 = (int)(lo >> 5);
   t->rec1 = hi > lo ? (int)((hi + 31) >> 5) : t->rec0;
-  t->parts = min(a.splits, max(1, (t->rec1 - t->rec0 + a.chunk - 1) / a.chunk));
+  t->units = max(1, (t->rec1 - t->rec0 + kWaves - 1) / kWaves);
   return true;
+}
+
+// o and lse of one row: four channels of the joined sum y, what it is divided
+// by, the reference.
+__device__ inline void store_row(const Args& a, const Tile& t, int D, int row, int d, float4v y, float sum, float ref) {
+  const int64_t at = (int64_t)(t.first + row / a.share) * (a.H * a.share) + t.h * a.share + row % a.share;
+  y *= sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (a.out_f32) {
+    *reinterpret_cast<float4v*>(static_cast<float*>(a.o) + at * D + d) = y;
+  } else {
+    const half4 z = {(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
+    *reinterpret_cast<half4*>(static_cast<uint16_t*>(a.o) + at * D + d) = z;
+  }
+  if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -__builtin_inff() : (ref + log2f(sum)) * kLn2;
+}
+
+// What crosses workgroups is stored and loaded at device scope, past the
+// caches of a die (sc1), so that no cache has to be written back or
+// invalidated: fences before and after the count cost 200 us a call, these 2.
+constexpr int kCoherent = 16;
+__device__ inline void put4(__amdgpu_buffer_rsrc_t r, int at, float4v v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, v), r, at, 0, kCoherent);
+}
+__device__ inline float4v get4(__amdgpu_buffer_rsrc_t r, int at) {
+  return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kCoherent));
+}
+
+// Even shares: the units of all tiles and heads in a line (tiles by qt, then
+// row, then head), of which workgroup w of W takes [T w / W, T (w + 1) / W).
+// A pair is a tile and row, qt * n_rows + row; up to 256 of them, up to four
+// beside each other in a lane.
+constexpr int kMaxPairs = 256;
+
+__device__ inline int share_start(int64_t T, int64_t w, int64_t W) { return (int)(T * w / W); }
+
+// Inclusive prefix sum over a wave.
+__device__ inline int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast 15 to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast 31 to rows 2 and 3
+  return x;
+}
+
+// A workgroup's share: units [unit, end) of T, the first of them unit `off` of
+// pair `pair`.  Every wave works it out for itself.
+struct Share {
+  int T, W, unit, end, pair, off;
+};
+__device__ inline Share share_of(const Args& a) {
+  const int lane = threadIdx.x & 63, pairs = a.n_rows * a.tiles, per = (pairs + 63) >> 6;
+  int n[kMaxPairs / 64], sum = 0;
+#pragma unroll
+  for (int e = 0; e < kMaxPairs / 64; ++e) {
+    const int i = lane * per + e;
+    n[e] = 0;
+    if (e < per && i < pairs) {
+      Tile t;
+      if (tile_of(a, i * a.H, &t)) n[e] = t.units * a.H;
+    }
+    sum += n[e];
+  }
+  const int incl = wave_scan(sum);
+  Share s;
+  s.T = __builtin_amdgcn_readlane(incl, 63);
+  s.W = min(a.shares, s.T);
+  s.unit = s.end = s.pair = s.off = 0;
+  if ((int)blockIdx.x >= s.W) return s;
+  s.unit = share_start(s.T, blockIdx.x, s.W);
+  s.end = share_start(s.T, blockIdx.x + 1, s.W);
+  // The last lane, then pair, that starts at or before the unit.
+  const int at = __popcll(__builtin_amdgcn_ballot_w64(incl - sum <= s.unit)) - 1;
+  s.pair = at * per;
+  s.off = s.unit - __builtin_amdgcn_readlane(incl - sum, at);
+#pragma unroll
+  for (int e = 0; e < kMaxPairs / 64 - 1; ++e) {
+    const int here = __builtin_amdgcn_readlane(n[e], at);
+    if (s.pair == at * per + e && s.off >= here) {
+      s.off -= here;
+      ++s.pair;
+    }
+  }
+  return s;
 }
 
 // Everything of a record that a lane needs, as it lies in memory.
@@ -101,76 +243,81 @@ struct Record {
   u4v kp[D / G][2], vp[D / G][2];
 };
 
-template <int D, int G, int QT>
-__global__ void __launch_bounds__(64 * kWaves) kv_attn_kernel(Args a) {
+// The kernel's arguments read anew: what a stretch of code needs of them holds
+// no scalar registers outside of it.  (All of them kept through the kernel,
+// with the state of the shares, spill 70 scalar registers.)
+__device__ inline Args args_anew() {
+  typedef const __attribute__((address_space(4))) Args* ptr;
+  ptr p = (ptr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const Args*)p;
+}
+
+// Waves a SIMD holds of a variant, as many as its registers allow without a
+// spill (512 / waves of them; past 256 half of them are accumulation registers
+// that cost moves).
+constexpr int waves_of(int D, int G) { return D == 64 ? 4 : D == 128 ? (G == 32 ? 2 : 3) : 1; }
+
+template <int D, int G>
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(waves_of(D, G))))
+kv_attn_kernel(Args args) {
   constexpr int NG = D / G, J = G / 32, KD = D / 32, VD = D / 16;
   constexpr int64_t kRec = 32 * (D + 8 * NG);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane >> 4, col = lane & 15;
-  const int tiles = a.H * a.n_rows * a.tiles;
-  const int part = blockIdx.x / tiles, id = blockIdx.x % tiles;
+  const int c = lane >> 4;
+  __shared__ float sm[kWaves][16], sl[kWaves][16];
+  __shared__ float so[kWaves][16][D + 4];
+  __shared__ int arrived;
+  Share share = {1, 1, 0, 1, 0, 0};
+  if (args.shares > 0) share = share_of(args);
+  const int first_unit = share.unit;
   Tile t;
-  if (!tile_of<QT>(a, id, &t) || part >= t.parts) return;
-  const int rec0 = t.rec0 + part * a.chunk;
-  const int rec1 = part == t.parts - 1 ? t.rec1 : rec0 + a.chunk;
-
-  // The lane's query rows as operands, their sums per group, their positions.
-  half8 q[QT][KD];
-  float qs[QT][NG];
-  int pos[QT];
-  const int64_t base = (int64_t)t.len - (a.cu ? (int64_t)a.cu[t.b + 1] - a.cu[t.b] : 1);
-  const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    const int row = t.row0 + 16 * u + col;
-    const bool in = row < t.rows;
-    const int tok = in ? row / a.share : 0, head = in ? t.h * a.share + row % a.share : 0;
-    const uint16_t* qp = a.q + (int64_t)(t.first + tok) * a.q_ts + head * a.q_hs;
-    pos[u] = in ? (int)max(base + tok, (int64_t)-1) : -1;
-#pragma unroll
-    for (int j = 0; j < KD; ++j) q[u][j] = in ? load8(qp + 32 * j + 8 * c) : zero;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float s = 0.0f;
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += (float)q[u][g * J + j][e];
-      s += __shfl_xor(s, 16);
-      s += __shfl_xor(s, 32);
-      qs[u][g] = s * a.scale_log2;
+  int h = 0;
+  bool fresh = true;   // the pair's tile is to be looked up
+  // The tiles, or parts of tiles, of the workgroup: one, or those of its share.
+  while (share.unit < share.end) {
+  const Args a = args_anew();
+  int rec0, rec1, head_unit = 0;
+  bool all_of_it = true;
+  const int slot = 2 * blockIdx.x + (share.unit != first_unit);
+  if (a.shares > 0) {
+    if (fresh) {
+      while (!tile_of(a, share.pair * a.H, &t)) ++share.pair;   // there is one: units are left
+      h = share.off / t.units;
+      share.off -= h * t.units;
     }
-  }
-  // The positions between which every row of the tile sees every token.
-  int all0 = 0, all1;
-  {
-    const int i0 = t.row0 / a.share, i1 = min(t.row0 + 16 * QT - 1, t.rows - 1) / a.share;
-    all1 = (int)max((int64_t)0, min((int64_t)t.len, base + i0 + 1));
-    if (a.window > 0) all0 = (int)max((int64_t)0, base + i1 + 1 - a.window);
-  }
-
-  float4v acc[QT][VD];
-  float macc[QT][NG], m[QT], l[QT];
-#pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    m[u] = -__builtin_inff();
-    l[u] = 0.0f;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) macc[u][g] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < VD; ++j) acc[u][j] = float4v{0, 0, 0, 0};
+    const int k0 = share.off, k1 = min(t.units, k0 + share.end - share.unit);
+    head_unit = share.unit - k0;
+    all_of_it = k0 == 0 && k1 == t.units;
+    rec0 = t.rec0 + kWaves * k0;
+    rec1 = min(t.rec1, t.rec0 + kWaves * k1);
+    share.unit += k1 - k0;
+    share.off = 0;
+    t.h = h;
+    fresh = ++h == a.H;
+    if (fresh) ++share.pair;
+  } else {
+    if (!tile_of(a, blockIdx.x, &t)) return;
+    rec0 = t.rec0;
+    rec1 = t.rec1;
+    share.unit = share.end;
   }
 
-  // The page of a record, -1 where there is none.
+  // The next record of the wave from `rec` on whose page the table names, as
+  // the address of its bytes; null where there is none.
   const int per_shift = a.page_shift - 5;
-  const int32_t* row_pages = a.pages + (int64_t)(t.len > 0 ? t.seq : 0) * a.max_pages;
-  auto page_at = [&](int rec) {
-    const int p = row_pages[rec >> per_shift];
-    return p >= 0 && p < a.n_pages ? p : -1;
+  const table_ptr row_pages = as_table(a.pages) + (int64_t)(t.len > 0 ? t.seq : 0) * a.max_pages;
+  auto next_record = [&](int* rec) -> const uint8_t* {
+    for (; *rec < rec1; *rec += kWaves) {
+      const int page = row_pages[*rec >> per_shift];
+      if (page >= 0 && page < a.n_pages) {
+        const int per = 1 << per_shift;
+        return a.layer + (int64_t)page * a.page_bytes + ((int64_t)t.h * per + (*rec & (per - 1))) * kRec;
+      }
+    }
+    return nullptr;
   };
-  auto load = [&](Record<D, G>& r, int rec, int page) {
-    const int per = 1 << per_shift;
-    const uint8_t* p = a.layer + (int64_t)page * a.page_bytes + ((int64_t)t.h * per + (rec & (per - 1))) * kRec;
+  auto load_k = [&](Record<D, G>& r, const uint8_t* p) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint8_t* kp = p + (64 * h + lane) * (D / 8);
@@ -187,292 +334,423 @@ __global__ void __launch_bounds__(64 * kWaves) kv_attn_kernel(Args a) {
         }
       }
     }
+  };
+  auto load_v = [&](Record<D, G>& r, const uint8_t* p) {
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) r.v[i] = *reinterpret_cast<const u4v*>(p + 16 * D + (64 * i + lane) * 16);
+  };
+  // The parameters of tokens 4c .. 4c + 3 and 16 more of the keys (first 0) or
+  // the values (first NG).
+  auto load_params = [&](u4v (&x)[NG][2], const uint8_t* p, int first) {
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        r.kp[g][h] = *reinterpret_cast<const u4v*>(p + 32 * D + g * 128 + (16 * h + 4 * c) * 4);
-        r.vp[g][h] = *reinterpret_cast<const u4v*>(p + 32 * D + (NG + g) * 128 + (16 * h + 4 * c) * 4);
-      }
+      for (int h = 0; h < 2; ++h)
+        x[g][h] = *reinterpret_cast<const u4v*>(p + 32 * D + (first + g) * 128 + (16 * h + 4 * c) * 4);
   };
 
-  auto compute = [&](const Record<D, G>& r, int rec) {
+  // The first record is on its way while the queries are set up.
+  Record<D, G> r;
+  int rec = rec0 + wave;
+  const uint8_t* at = next_record(&rec);
+  if (at != nullptr) {
+    load_k(r, at);
+    load_params(r.kp, at, 0);
+    load_params(r.vp, at, NG);
+    load_v(r, at);
+  }
+
+  // The lane's query rows as operands, their sums per group (and 8 times
+  // them, what codes less 8 lack) in the codes' unit, their positions.
+  int qx = threadIdx.x;
+  asm volatile("" : "+v"(qx));   // as above the join, below
+  const int qc = (qx >> 4) & 3, qcol = qx & 15;
+  half8 q[KD];
+  float qs[NG];
+  float4v q8[NG];
+  int pos;
+  const int64_t base = (int64_t)t.len - t.asked;
+  const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  const int row = t.row0 + qcol;
+  const bool in = row < t.rows;
+  const int tok = in ? row / a.share : 0, head = in ? t.h * a.share + row % a.share : 0;
+  const uint16_t* qp = a.q + (int64_t)(t.first + tok) * a.q_ts + head * a.q_hs;
+  pos = in ? (int)max(base + tok, (int64_t)-1) : -1;
+#pragma unroll
+  for (int j = 0; j < KD; ++j) q[j] = in ? load8(qp + 32 * j + 8 * qc) : zero;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += (float)q[g * J + j][e];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    qs[g] = s / kCodeUnit;
+    const float s8 = 8.0f / kCodeUnit * s;
+    q8[g] = float4v{s8, s8, s8, s8};
+  }
+  // The positions between which every row of the tile sees every token.
+  int all0 = 0, all1;
+  {
+    const int i0 = t.row0 / a.share, i1 = min(t.row0 + 16 - 1, t.rows - 1) / a.share;
+    all1 = (int)max((int64_t)0, min((int64_t)t.len, base + i0 + 1));
+    if (a.window > 0) all0 = (int)max((int64_t)0, base + i1 + 1 - a.window);
+  }
+
+  const float logit = a.scale_log2 * kCodeUnit;
+
+  // A row's state: its reference r, above which a logit makes it grow (never
+  // before it has seen one: then any does), sums of exp2(s - r).
+  const float kNone = -3.0e38f;
+  float4v acc[VD];
+  float macc[NG], ref, grow, l;
+  bool low;   // the row has seen a large value scale
+  ref = 0.0f;
+  low = false;
+  grow = kNone;
+  l = 0.0f;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) macc[g] = 0.0f;
+#pragma unroll
+  for (int j = 0; j < VD; ++j) acc[j] = float4v{0, 0, 0, 0};
+  auto rescale = [&](float f) {
+    l *= f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) macc[g] *= f;
+#pragma unroll
+    for (int j = 0; j < VD; ++j) acc[j] *= f;
+  };
+
+  while (at != nullptr) {
+    // A register's record is replaced by the next one's as soon as it is used,
+    // so that a load has nearly a whole pass to arrive in.
+    int rec_n = rec + kWaves;
+    const uint8_t* at_n = next_record(&rec_n);
+    const uint8_t* pf = at_n != nullptr ? at_n : at;
     const bool whole = rec * 32 >= all0 && rec * 32 + 32 <= all1;
     half8 kf[2][KD];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int j = 0; j < KD; ++j) kf[h][j] = code_operand(r.k[h][j]);
-    half8 hi[QT][NG], lo[QT][NG];
+    uint32_t scales = 0;
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      float s[2][4];
+    for (int g = 0; g < NG; ++g)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x[4] = {0, 0, 0, 0}, y[4] = {0, 0, 0, 0};
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          float4v z = {0, 0, 0, 0};
+        for (int i = 0; i < 4; ++i) scales |= r.vp[g][h][i];
+    u4v hi[NG], lo[NG];
+    float s[2][4];
 #pragma unroll
-          for (int j = 0; j < J; ++j) z = mfma(kf[h][g * J + j], q[u][g * J + j], z);
+    for (int h = 0; h < 2; ++h) {
+      float x[4] = {0, 0, 0, 0};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float sk = lo_half(r.kp[g][h][i]);
-            x[i] = fmaf(sk, z[i], x[i]);
-            y[i] = fmaf(centred(sk, hi_half(r.kp[g][h][i])), qs[u][g], y[i]);
-          }
+      for (int g = 0; g < NG; ++g) {
+        float4v z = q8[g];
+#pragma unroll
+        for (int j = 0; j < J; ++j) z = mfma(kf[h][g * J + j], q[g * J + j], z);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const half2v p = pair(r.kp[g][h][i]);
+          x[i] = fmaf((float)p[0], z[i], x[i]);
+          x[i] = fmaf((float)p[1], qs[g], x[i]);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][i] = fmaf(x[i], a.scale_log2, y[i]);
       }
-      uint32_t seen = 0xFFu;
-      if (!whole) {
-        seen = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+      for (int i = 0; i < 4; ++i) s[h][i] = fmaf(x[i], logit, -ref);
+    }
+    load_k(r, pf);
+    u4v vp[NG][2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int at = rec * 32 + 16 * h + 4 * c + i;
-            const bool see = at <= pos[u] && (a.window <= 0 || at > pos[u] - a.window);
-            seen |= (uint32_t)see << (4 * h + i);
-            if (!see) s[h][i] = -__builtin_inff();
-          }
-      }
-      float top = s[0][0];
+    for (int g = 0; g < NG; ++g)
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
-      if (__builtin_amdgcn_ballot_w64(top > m[u]) != 0) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = fmaxf(top, m[u]);
-        const float f = now == -__builtin_inff() ? 1.0f : exp2f(m[u] - now);
-        m[u] = now;
-        l[u] *= f;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) macc[u][g] *= f;
-#pragma unroll
-        for (int j = 0; j < VD; ++j) acc[u][j] *= f;
-      }
-      const float ref = m[u] == -__builtin_inff() ? 0.0f : m[u];
-      float p[2][4];
+      for (int h = 0; h < 2; ++h) vp[g][h] = r.vp[g][h];
+    uint32_t any = scales;
+    if (!whole) {
+      any = 0;
+      asm volatile("");   // a branch: as selects the masks cost every record 40 instructions
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[h][i] = __builtin_amdgcn_exp2f(s[h][i] - ref);
-          l[u] += p[h][i];
-        }
+          const int tok = rec * 32 + 16 * h + 4 * c + i;
+          const bool see = tok <= pos && (a.window <= 0 || tok > pos - a.window);
+          if (!see) s[h][i] = -__builtin_inff();
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        float w[2][4];
+          for (int g = 0; g < NG; ++g) {
+            vp[g][h][i] = see ? vp[g][h][i] : 0u;   // may be anything
+            any |= vp[g][h][i];
+          }
+        }
+    }
+    // A row's first value scale of 2 or more (or NaN) among the tokens it sees.
+    if (__builtin_amdgcn_ballot_w64((any & 0x4000u) != 0 && !low) != 0) {
+      any |= __shfl_xor(any, 16);
+      any |= __shfl_xor(any, 32);
+      if ((any & 0x4000u) != 0 && !low) {
+        low = true;
+        if (grow != kNone) {
+          ref += kHigh - kLow;
+          grow = kLow;
+          rescale(exp2f(kLow - kHigh));
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[h][i] -= kHigh - kLow;
+        }
+      }
+    }
+    float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    if (__builtin_amdgcn_ballot_w64(top > grow) != 0) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (top > grow) {
+        const float by = top - (low ? kLowSet : kHighSet);
+        ref += by;
+        rescale(grow == kNone ? 0.0f : exp2f(-by));
+        grow = low ? kLow : kHigh;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float sv = lo_half(r.vp[g][h][i]), mv = centred(sv, hi_half(r.vp[g][h][i]));
-            if (!whole && !((seen >> (4 * h + i)) & 1)) sv = mv = 0.0f;   // what no row may see may be anything
-            w[h][i] = p[h][i] * sv;
-            macc[u][g] = fmaf(p[h][i], mv, macc[u][g]);
-          }
-        // Operand register i: tokens 4c + i and 16 + 4c + i.
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const _Float16 x = (_Float16)w[h][i];
-            hi[u][g][2 * i + h] = x;
-            lo[u][g][2 * i + h] = (_Float16)(w[h][i] - (float)x);
-          }
+          for (int i = 0; i < 4; ++i) s[h][i] -= by;
       }
     }
+    float p[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[h][i] = __builtin_amdgcn_exp2f(s[h][i]);
+        l += p[h][i];
+      }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      // Operand register i: tokens 4c + i and 16 + 4c + i.
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const half2v v = pair(vp[g][h][i]);
+          w[h] = fmaf(p[h][i], (float)v[0], 0.0f);   // one instruction with the fp16 operand as it is
+          macc[g] = fmaf(p[h][i], fmaf(8.0f, (float)v[0], (float)v[1]), macc[g]);
+        }
+        const uint32_t x = cut(w[0], w[1]);
+        hi[g][i] = x;
+        lo[g][i] = cut(rest0(x, w[0]), rest1(x, w[1]));
+      }
+    }
+    load_params(r.kp, pf, 0);
+    load_params(r.vp, pf, NG);
 #pragma unroll
     for (int j = 0; j < VD; ++j) {
       const half8 vf = code_operand(r.v[j >> 2][j & 3]);
-#pragma unroll
-      for (int u = 0; u < QT; ++u) {
-        acc[u][j] = mfma(vf, hi[u][j * 16 / G], acc[u][j]);
-        acc[u][j] = mfma(vf, lo[u][j * 16 / G], acc[u][j]);
-      }
+      acc[j] = mfma(vf, __builtin_bit_cast(half8, hi[j * 16 / G]), acc[j]);
+      acc[j] = mfma(vf, __builtin_bit_cast(half8, lo[j * 16 / G]), acc[j]);
     }
-  };
-
-  if constexpr (D == 256) {
-    for (int rec = rec0 + wave; rec < rec1; rec += kWaves) {
-      const int page = page_at(rec);
-      if (page < 0) continue;
-      Record<D, G> cur;
-      load(cur, rec, page);
-      compute(cur, rec);
-    }
-  } else {
-    Record<D, G> cur, nxt;
-    int rec = rec0 + wave, page = -1, page_n = -1;
-    if (rec < rec1) {
-      page = page_at(rec);
-      if (page >= 0) load(cur, rec, page);
-    }
-    while (rec < rec1) {
-      const int next = rec + kWaves;
-      if (next < rec1) {
-        page_n = page_at(next);
-        if (page_n >= 0) load(nxt, next, page_n);
-      }
-      if (page >= 0) compute(cur, rec);
-      cur = nxt;
-      page = page_n;
-      rec = next;
-    }
+    load_v(r, pf);
+    at = at_n;
+    rec = rec_n;
   }
 
-  // Join the four lane groups' sums, then the waves.
-  __shared__ float sm[kWaves][16], sl[kWaves][16];
-  __shared__ float so[kWaves][16][D + 4];
+  // Join the four lane groups' sums, then the waves.  A row that has seen
+  // nothing has the reference -infinity from here on.
+  // (The thread's number is taken anew, so that what only this part needs of it
+  // holds no registers meanwhile.)
+  int tx = threadIdx.x;
+  asm volatile("" : "+v"(tx));
+  const Args z = args_anew();
+  const __amdgpu_buffer_rsrc_t parts_of =
+      __builtin_amdgcn_make_buffer_rsrc(z.part, 0, 2 * z.shares * z.R * (D + 4) * 4, 0x00020000);
+  const int oc = (tx >> 4) & 3, ocol = tx & 15;
+  const float m = grow == kNone ? -__builtin_inff() : ref;
+  float L = l;
+  L += __shfl_xor(L, 16);
+  L += __shfl_xor(L, 32);
+  float M[NG];
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    float L = l[u];
-    L += __shfl_xor(L, 16);
-    L += __shfl_xor(L, 32);
-    float M[NG];
+  for (int g = 0; g < NG; ++g) {
+    M[g] = macc[g] + __shfl_xor(macc[g], 16);
+    M[g] += __shfl_xor(M[g], 32);
+  }
+  __syncthreads();   // what was joined before has been read
+  if (oc == 0) sm[wave][ocol] = m;
+  __syncthreads();
+  float top = sm[0][ocol];
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      M[g] = macc[u][g] + __shfl_xor(macc[u][g], 16);
-      M[g] += __shfl_xor(M[g], 32);
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm[w][ocol]);
+  const float f = m == -__builtin_inff() ? 0.0f : exp2f(m - top);
+  if (oc == 0) sl[wave][ocol] = L * f;
+#pragma unroll
+  for (int j = 0; j < VD; ++j) {
+    float4v y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = fmaf(acc[j][i], kCodeUnit, M[j * 16 / G]) * f;
+    *reinterpret_cast<float4v*>(&so[wave][ocol][16 * j + 4 * oc]) = y;
+  }
+  __syncthreads();
+  for (int i = tx; i < 16 * D / 4; i += 64 * kWaves) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4, row = t.row0 + r;
+    if (row >= t.rows) continue;
+    float4v y = *reinterpret_cast<float4v*>(&so[0][r][d]);
+    float sum = sl[0][r], most = sm[0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+      y += *reinterpret_cast<float4v*>(&so[w][r][d]);
+      sum += sl[w][r];
+      most = fmaxf(most, sm[w][r]);
     }
-    if (u > 0) __syncthreads();
-    if (c == 0) sm[wave][col] = m[u];
-    __syncthreads();
-    float top = sm[0][col];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm[w][col]);
-    const float f = m[u] == -__builtin_inff() ? 0.0f : exp2f(m[u] - top);
-    if (c == 0) sl[wave][col] = L * f;
-#pragma unroll
-    for (int j = 0; j < VD; ++j) {
-      float4v y;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = (acc[u][j][i] + M[j * 16 / G]) * f;
-      *reinterpret_cast<float4v*>(&so[wave][col][16 * j + 4 * c]) = y;
+    if (all_of_it) {
+      store_row(z, t, D, row, d, y, sum, most);
+    } else {
+      const int p = (slot * z.R + r) * (D + 4) * 4;
+      put4(parts_of, p + 4 * d, y);
+      if (d == 0) put4(parts_of, p + 4 * D, float4v{most, sum, 0, 0});
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * kWaves) {
-      const int r = i / (D / 4), d = i % (D / 4) * 4, row = t.row0 + 16 * u + r;
-      if (row >= t.rows) continue;
-      float4v y = *reinterpret_cast<float4v*>(&so[0][r][d]);
-      float sum = sl[0][r], most = sm[0][r];
+  }
+  if (all_of_it) continue;
+
+  // The last workgroup of a tile to leave its part joins them all, in the
+  // order of the parts; where there are many, the last one of each group of
+  // them joins the group into its first part, and the last group the groups.
+  // Who finds a count full sets it back to 0.
+  const int64_t T = share.T, W = share.W, u0 = head_unit, u1 = u0 + t.units - 1;
+  const int w0 = (int)(((u0 + 1) * W - 1) / T), parts = (int)(((u1 + 1) * W - 1) / T) - w0 + 1;
+  // Workgroup w0 comes to the tile after others unless its share starts there.
+  const int skip = share_start(T, w0, W) != u0;
+  auto slot_of = [&](int k) { return 2 * (w0 + k) + (k == 0 ? skip : 0); };
+  const int g = parts > kOneLevel ? (int)ceilf(sqrtf((float)parts)) : parts, groups = (parts + g - 1) / g;
+  int first = ((int)blockIdx.x - w0) / g * g, step = 1, n = min(g, parts - first);
+  int32_t* count = z.count + slot_of(first);
+  for (;;) {
+  __builtin_amdgcn_s_waitcnt(0);   // what is joined has arrived
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int before = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before == n - 1) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    arrived = before;
+  }
+  __syncthreads();
+  if (arrived != n - 1) break;
+  const bool last = step != 1 || groups == 1;
+  asm volatile("" : "+v"(tx)::"memory");
+  // D/4 lanes take a row, or each `per` of NGRP groups of them some of its parts.
+  constexpr int kAhead = D == 64 ? 4 : 8;   // parts in flight a lane, as the registers allow
+  constexpr int kLanes = D / 4, NGRP = 64 * kWaves / kLanes;
+  const int rows = min(16, t.rows - t.row0), per = max(1, NGRP / rows);
+  const int grp = tx / kLanes, d = tx % kLanes * 4;
+  float(*jy)[D + 4] = so[0];   // NGRP <= 16 rows of it
+  for (int r0 = 0; r0 < rows; r0 += NGRP / per) {
+    const int r = r0 + grp / per, sub = grp % per;
+    float ref = -__builtin_inff(), sum = 0.0f;
+    float4v y = {0, 0, 0, 0};
+    if (r < rows && grp < NGRP / per * per) {
+      for (int s = sub; s < n; s += kAhead * per) {
+        float4v v[kAhead];
+        float m[kAhead], l[kAhead];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        y += *reinterpret_cast<float4v*>(&so[w][r][d]);
-        sum += sl[w][r];
-        most = fmaxf(most, sm[w][r]);
-      }
-      if (t.parts > 1) {
-        float* p = a.part + (((int64_t)id * a.splits + part) * a.R + 16 * u + r) * (D + 4);
-        *reinterpret_cast<float4v*>(p + d) = y;
-        if (d == 0) {
-          p[D] = most;
-          p[D + 1] = sum;
+        for (int e = 0; e < kAhead; ++e) {
+          const int k = first + step * min(s + e * per, n - 1);
+          const int p = (slot_of(k) * z.R + r) * (D + 4) * 4;
+          v[e] = get4(parts_of, p + 4 * d);
+          const float4v x = get4(parts_of, p + 4 * D);
+          m[e] = x[0];
+          l[e] = x[1];
         }
-        continue;
+        float top = ref;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+          if (s + e * per < n) top = fmaxf(top, m[e]);
+        const float f = ref == -__builtin_inff() ? 0.0f : exp2f(ref - top);
+        sum *= f;
+        y *= f;
+        ref = top;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+          if (s + e * per < n) {
+            const float g = m[e] == -__builtin_inff() ? 0.0f : exp2f(m[e] - top);
+            sum = fmaf(l[e], g, sum);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = fmaf(v[e][i], g, y[i]);
+          }
       }
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      const int64_t at = (int64_t)(t.first + row / a.share) * (a.H * a.share) + t.h * a.share + row % a.share;
-      y *= inv;
-      if (a.out_f32) {
-        *reinterpret_cast<float4v*>(static_cast<float*>(a.o) + at * D + d) = y;
+    }
+    __syncthreads();   // so has been read
+    if (grp < NGRP) {
+      *reinterpret_cast<float4v*>(&jy[grp][d]) = y;
+      if (d == 0) {
+        jy[grp][D] = ref;
+        jy[grp][D + 1] = sum;
+      }
+    }
+    __syncthreads();
+    if (r < rows && sub == 0 && grp < NGRP / per * per) {
+      float top = ref;
+      for (int e = 1; e < per; ++e) top = fmaxf(top, jy[grp + e][D]);
+      const float f = ref == -__builtin_inff() ? 0.0f : exp2f(ref - top);
+      sum *= f;
+      y *= f;
+      for (int e = 1; e < per; ++e) {
+        const float m = jy[grp + e][D], g = m == -__builtin_inff() ? 0.0f : exp2f(m - top);
+        sum = fmaf(jy[grp + e][D + 1], g, sum);
+        const float4v v = *reinterpret_cast<float4v*>(&jy[grp + e][d]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], g, y[i]);
+      }
+      if (last) {
+        store_row(z, t, D, t.row0 + r, d, y, sum, top);
       } else {
-        const half4 z = {(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
-        *reinterpret_cast<half4*>(static_cast<uint16_t*>(a.o) + at * D + d) = z;
+        const int p = (slot_of(first) * z.R + r) * (D + 4) * 4;
+        put4(parts_of, p + 4 * d, y);
+        if (d == 0) put4(parts_of, p + 4 * D, float4v{top, sum, 0, 0});
       }
-      if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -__builtin_inff() : (most + log2f(sum)) * kLn2;
     }
   }
-}
-
-// Joins the parts of a tile's rows: a wave per row.
-template <int D, int QT>
-__global__ void __launch_bounds__(256) kv_join_kernel(Args a) {
-  const int id = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  Tile t;
-  if (!tile_of<QT>(a, id, &t) || t.parts == 1) return;
-  const int row = t.row0 + r;
-  if (r >= 16 * QT || row >= t.rows) return;
-  const float* p = a.part + ((int64_t)id * a.splits * a.R + r) * (D + 4);
-  const int64_t step = (int64_t)a.R * (D + 4);
-  float top = -__builtin_inff();
-  for (int s = lane; s < t.parts; s += 64) top = fmaxf(top, p[s * step + D]);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float sum = 0.0f, y[D / 64];
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) y[e] = 0.0f;
-  for (int s = 0; s < t.parts; ++s) {
-    const float m = p[s * step + D];
-    const float f = m == -__builtin_inff() ? 0.0f : exp2f(m - top);
-    sum = fmaf(p[s * step + D + 1], f, sum);
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) y[e] = fmaf(p[s * step + 64 * e + lane], f, y[e]);
+  if (last) break;
+  count = z.count + 2 * kMaxShares + slot_of(0);
+  step = g;
+  n = groups;
+  first = 0;
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const int64_t at = (int64_t)(t.first + row / a.share) * (a.H * a.share) + t.h * a.share + row % a.share;
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) {
-    if (a.out_f32)
-      static_cast<float*>(a.o)[at * D + 64 * e + lane] = y[e] * inv;
-    else
-      static_cast<_Float16*>(a.o)[at * D + 64 * e + lane] = (_Float16)(y[e] * inv);
   }
-  if (a.lse && lane == 0) a.lse[at] = sum == 0.0f ? -__builtin_inff() : (top + log2f(sum)) * kLn2;
 }
 
 // The split of a call.  Everything here comes from the caller's sizes; the
 // lengths themselves are on the device.
 struct Plan {
-  int qt, tiles, splits, chunk, R;
+  int tiles, shares, R;
   int64_t ids;
 };
 
 bool plan(const KvDev& c, const AttnCall& a, Plan* p) {
-  const int64_t share = a.n_heads / c.H, rows = (int64_t)a.max_q * share;
-  // More rows a tile would not fit the registers: 4 tiles of 16 at D = 64, 2
-  // at D = 128, 1 at D = 256, where the next record is not fetched ahead
-  // either.  No variant spills: one that did gave wrong sums.
-  const int most = 256 / c.D;
-  p->qt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  if (p->qt > most) p->qt = most;
-  const int64_t tiles = (rows + 16 * p->qt - 1) / (16 * p->qt);
-  p->ids = tiles * c.H * a.n_rows;
+  const int64_t rows = (int64_t)a.max_q * (a.n_heads / c.H), tiles = (rows + 15) / 16, pairs = tiles * a.n_rows;
+  p->ids = pairs * c.H;
   if (p->ids > (1 << 23)) return false;   // a launch has fewer than 2^32 threads
   p->tiles = (int)tiles;
-  p->R = (int)(rows < 16 * p->qt ? rows : 16 * p->qt);
-  int64_t len = a.max_len > 0 ? a.max_len : (int64_t)c.max_pages * c.page_size;
+  p->R = (int)(rows < 16 ? rows : 16);
+  const int64_t room = (int64_t)c.max_pages * c.page_size;
+  int64_t len = a.max_len > 0 ? a.max_len : room;
   if (a.window > 0 && len > (int64_t)a.window + a.max_q) len = (int64_t)a.window + a.max_q;
-  const int64_t recs = (len + 31) / 32 + 1;
-  // Parts of 16 records (four a wave) at least, and no more workgroups than
-  // about 2048.
-  int64_t splits = (2048 + p->ids - 1) / p->ids;
-  if (splits > (recs + 15) / 16) splits = (recs + 15) / 16;
-  if (splits < 1) splits = 1;
-  if (splits > 1024) splits = 1024;
-  p->splits = (int)splits;
-  p->chunk = (int)((recs + splits - 1) / splits);
+  const int64_t unit = 32 * kWaves, units = (len + unit - 1) / unit, slots = kCus * waves_of(c.D, c.G);
+  p->shares = 0;
+  // The line of units is counted in 31 bits, whatever the lengths are.
+  if (pairs <= kMaxPairs && units > kMinUnits && (room / unit + 2) * p->ids < (1 << 30)) {
+    const int64_t all = (units * p->ids + kUnitsOfShare - 1) / kUnitsOfShare;
+    p->shares = (int)(all < slots ? all : slots);
+  }
   return true;
 }
 
-template <int D, int G, int QT>
-void start(const Args& a, const Plan& p, hipStream_t s) {
-  kv_attn_kernel<D, G, QT><<<(uint32_t)(p.ids * p.splits), 64 * kWaves, 0, s>>>(a);
-  if (p.splits > 1) kv_join_kernel<D, QT><<<dim3((uint32_t)p.ids, (p.R + 3) / 4), 256, 0, s>>>(a);
-}
+// Two counts for each of the two parts that a share can leave.
+constexpr size_t kCountBytes = 4 * (2 + 2) * kMaxShares;
 
 template <int D, int G>
-void start_qt(const Args& a, const Plan& p, hipStream_t s) {
-  if (p.qt == 1) start<D, G, 1>(a, p, s);
-  if constexpr (D <= 128)
-    if (p.qt == 2) start<D, G, 2>(a, p, s);
-  if constexpr (D == 64)
-    if (p.qt == 4) start<D, G, 4>(a, p, s);
+void start(const Args& a, const Plan& p, hipStream_t s) {
+  kv_attn_kernel<D, G><<<(uint32_t)(p.shares ? p.shares : p.ids), 64 * kWaves, 0, s>>>(a);
 }
 
 }  // namespace
@@ -480,7 +758,7 @@ void start_qt(const Args& a, const Plan& p, hipStream_t s) {
 bool kv_attention_plan(const KvDev& c, const AttnCall& a, size_t* ws_bytes) {
   Plan p;
   if (!plan(c, a, &p)) return false;
-  *ws_bytes = p.splits > 1 ? (size_t)(p.ids * p.splits * p.R) * (c.D + 4) * 4 : 0;
+  *ws_bytes = p.shares > 0 ? kCountBytes + (size_t)2 * p.shares * p.R * (c.D + 4) * 4 : 0;
   return true;
 }
 
@@ -496,7 +774,8 @@ hipError_t launch_kv_attention(const KvDev& c, int layer, const AttnCall& call, 
   a.q = call.q.p;
   a.o = call.o;
   a.lse = call.lse;
-  a.part = static_cast<float*>(call.ws);
+  a.count = static_cast<int32_t*>(call.ws);
+  a.part = call.ws != nullptr ? reinterpret_cast<float*>(static_cast<uint8_t*>(call.ws) + kCountBytes) : nullptr;
   a.q_ts = call.q.ts;
   a.q_hs = call.q.hs;
   a.page_bytes = c.page_bytes;
@@ -512,16 +791,15 @@ hipError_t launch_kv_attention(const KvDev& c, int layer, const AttnCall& call, 
   a.max_pages = c.max_pages;
   a.n_pages = c.n_pages;
   a.tiles = p.tiles;
-  a.splits = p.splits;
-  a.chunk = p.chunk;
+  a.shares = p.shares;
   a.R = p.R;
   a.out_f32 = call.out_f32;
   if (c.D == 64) {
-    c.G == 32 ? start_qt<64, 32>(a, p, s) : start_qt<64, 64>(a, p, s);
+    c.G == 32 ? start<64, 32>(a, p, s) : start<64, 64>(a, p, s);
   } else if (c.D == 128) {
-    c.G == 32 ? start_qt<128, 32>(a, p, s) : c.G == 64 ? start_qt<128, 64>(a, p, s) : start_qt<128, 128>(a, p, s);
+    c.G == 32 ? start<128, 32>(a, p, s) : c.G == 64 ? start<128, 64>(a, p, s) : start<128, 128>(a, p, s);
   } else {
-    c.G == 32 ? start_qt<256, 32>(a, p, s) : c.G == 64 ? start_qt<256, 64>(a, p, s) : start_qt<256, 128>(a, p, s);
+    c.G == 32 ? start<256, 32>(a, p, s) : c.G == 64 ? start<256, 64>(a, p, s) : start<256, 128>(a, p, s);
   }
   return hipGetLastError();
 }

@@ -206,8 +206,8 @@ __global__ void __launch_bounds__(64 * kWaves) q4_gemm_kernel(const uint8_t* __r
         float s[4], m[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[i] = lo_half(d.p[rt][g][i]);
-          m[i] = centred(s[i], hi_half(d.p[rt][g][i]));
+          m[i] = centred(lo_half(d.p[rt][g][i]), hi_half(d.p[rt][g][i]));
+          s[i] = lo_half(d.p[rt][g][i]) * kCodeUnit;
         }
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {

@@ -7,6 +7,7 @@ library's kernels.  There is no fallback: if libtq.so is missing, every call
 raises.
 """
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -666,7 +667,7 @@ class KVCache:
     calls below.  One cache serves one stream at a time: calls on another
     one are the caller's to order."""
 
-    __slots__ = ("data", "pages", "lens", "refs", "n_kv_heads", "head_dim", "page_size", "group", "_c", "_ref")
+    __slots__ = ("data", "pages", "lens", "refs", "n_kv_heads", "head_dim", "page_size", "group", "_ref", "_attn_ws")
 
     def __init__(self, data, pages, lens, refs, n_kv_heads, head_dim, page_size=64, group=64):
         _cuda(data, torch.uint8, "data")
@@ -685,7 +686,8 @@ class KVCache:
             raise ValueError(f"a page has {want} bytes")
         self.data, self.pages, self.lens, self.refs = data, pages, lens, refs
         self.n_kv_heads, self.head_dim, self.page_size, self.group = n_kv_heads, head_dim, page_size, group
-        self._c, self._ref = c, ref
+        self._ref = ref
+        self._attn_ws = {}   # stream -> workspace of tq_kv_attention, zeros when made
 
     @classmethod
     def empty(cls, n_layers, n_pages, n_seqs, max_pages, n_kv_heads, head_dim, page_size=64, group=64,
@@ -699,6 +701,17 @@ class KVCache:
         return cls(torch.empty((n_layers, n_pages, pb), dtype=torch.uint8, device=device),
                    torch.full((n_seqs, max_pages), -1, **i32), torch.zeros(n_seqs, **i32), torch.zeros(n_pages, **i32),
                    n_kv_heads, head_dim, page_size, group)
+
+    def attention_workspace(self, need, stream=None):
+        """A workspace of at least `need` bytes for tq_kv_attention on a stream
+        (the current one without): one per stream, kept with the cache and
+        made anew, larger, when a call needs more."""
+        key = _stream(stream)
+        ws = self._attn_ws.get(key)
+        if ws is None or ws.numel() < need:
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                ws = self._attn_ws[key] = torch.zeros(need, dtype=torch.uint8, device=self.data.device)
+        return ws
 
     def _buffers(self):
         return self.data, self.pages, self.lens, self.refs
@@ -826,7 +839,8 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=1, max_len=0, s
                     lse=None, out_f32=False, want_lse=False, workspace=None, stream=None):
     """Attention of q [T, n_heads, D], the last tokens of their slots, over the
     cache: o [T, n_heads, D] (fp16 or fp32), and with want_lse also the log of
-    the softmax's sum, fp32 [T, n_heads].  scale: 1 / sqrt(D) without."""
+    the softmax's sum, fp32 [T, n_heads].  scale: 1 / sqrt(D) without.  A
+    workspace of the caller's is zeros before its first call."""
     T, n_heads, D = q.shape
     n = seqs.numel() if seqs is not None else (cu_q.numel() - 1 if cu_q is not None else T)
     if cu_q is None and n != T:
@@ -847,7 +861,10 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=1, max_len=0, s
                  o.data_ptr(), None if lse is None else lse.data_ptr(), None, 0)
     need = lib().tq_kv_attention_workspace_bytes(cache._ref, a)
     if need:
-        workspace = _workspace(workspace, need, q.device)
+        if workspace is None:
+            workspace = cache.attention_workspace(need, stream)
+        else:
+            _cuda(workspace, torch.uint8, "workspace")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
     _check(lib().tq_kv_attention(cache._ref, layer, a, _stream(stream)), "tq_kv_attention")
     _used_on(stream, q, seqs, cu_q, o, lse, workspace, *cache._buffers())
