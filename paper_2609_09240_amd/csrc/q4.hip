@@ -3,20 +3,34 @@
 //     y[b][n] = sum_g ( s sum_{k in g} q x[b][k]  +  m sum_{k in g} x[b][k] )
 //
 // One matrix instruction v_mfma_f32_16x16x32_f16 takes 16 rows of W (the
-// codes less 8, exact in fp16; the offsets grow by 8 scales) and 16 rows of X over 32 inputs, for one
+// codes less 8, exact in fp16) and 16 rows of X over 32 inputs, for one
 // activation row as for sixteen: columns past B repeat row B-1 and are
-// dropped.  The codes of a group are summed in a chain of their own, and the
-// group's scale multiplies the fp32 sums, four per lane, so no weight is
-// formed and nothing is rounded below fp32.  The sum of x is one more
-// instruction per 32 inputs with ones in place of the codes, shared by the
-// row tiles of a wave.
+// dropped.  The codes of a group are summed in a chain of their own, which
+// starts at 8 times the group's sum of x, and the group's scale and offset
+// multiply fp32 sums, four per lane, so no weight is formed and nothing is
+// rounded below fp32.  The sum of x is one more instruction per 32 inputs with
+// constants in place of the codes, shared by the row tiles of a wave.
+//
+// Two kernels.  With few rows of X every wave streams blocks of 128 inputs of
+// its row tiles straight into registers and reads X as operands from the
+// caches; a load of X then touches a line per row, and from 5 rows on (3 where
+// there are many row tiles) that costs more than staging X in LDS, which the
+// other kernel does.  Kernel times, weights from HBM, groups of 128:
+//   1024 x 4096     B = 1 4.3 us (launch and two trips to memory)
+//   4096 x 4096     B = 1 4.6
+//   4096 x 12288    B = 1 8.8, 3 8.9, 8 11.0, 16 11.2, 32 20.1, 64 39.4
+//   12288 x 4096    B = 1 8.6, 4 9.7, 16 10.2, 32 13.6, 64 25.2
+//   131072 x 4096   B = 1 53.8 (groups of 64: 302 MB, 5.6 TB/s), 16 76
+// B = 1 of a large matrix is bound by HBM; the small ones by latency; from B =
+// 16 on by X, which every workgroup reads whole (64 rows of 12288: 1.6 MB for
+// two row tiles; splitting K over workgroups would share it).
+
+#include <atomic>
 
 #include "q4_internal.h"
 
 namespace tq {
 namespace {
-
-constexpr int kWaves = 8;
 
 __device__ inline float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -107,10 +121,9 @@ __global__ void __launch_bounds__(256) q4_unpack_kernel(const uint32_t* __restri
 // y[b][n] as the sum of x times the weights formed one by one: for outputs
 // that are not finite, where the sums over codes are not what the weights
 // give (an infinite input times a code of 0).
-__device__ __attribute__((noinline)) float by_weights(const uint8_t* codes, const uint16_t* params, int K, int KB,
+__device__ __attribute__((noinline)) float by_weights(const uint8_t* codes, const uint32_t* pw, int K, int KB,
                                                       int G, const uint16_t* x, int64_t n) {
   const uint32_t* cw = reinterpret_cast<const uint32_t*>(codes);
-  const uint32_t* pw = reinterpret_cast<const uint32_t*>(params);
   const int64_t T = n >> 4;
   const int r = (int)(n & 15);
   float acc = 0.0f;
@@ -131,133 +144,81 @@ __device__ inline half8 load_tail(const uint16_t* x, int k, int K) {
   return v;
 }
 
-template <int G, int RT, int CT>
-struct Block {
-  u4v w[RT];
-  u4v p[RT][128 / G];
-  half8 x[CT][4];
-};
+// The parameters of a row tile and block are one word a lane: lane (c, k) holds
+// row 4 c + k % 4 of group k / 4, and a broadcast within 16 lanes brings each to
+// the lanes whose sums it scales.
+template <int NG>
+__device__ inline const uint32_t* param_lane(const uint32_t* params, int64_t T, int KB) {
+  const int c = (threadIdx.x >> 4) & 3, k = threadIdx.x & 15;
+  return params + T * KB * NG * 16 + (k / 4 % NG) * 16 + 4 * c + (k & 3);
+}
 
-template <int G, int RT, int CT>
-__global__ void __launch_bounds__(64 * kWaves) q4_gemm_kernel(const uint8_t* __restrict__ codes,
-                                                              const uint16_t* __restrict__ params,
-                                                              const uint16_t* __restrict__ X, int64_t ldx, int N,
-                                                              int K, int B, void* __restrict__ Y, int out_f32) {
+// One block of 128 inputs of RT row tiles times CT tiles of 16 rows of X, added
+// to acc, in the codes' unit.  done(rt) is called once the registers of row
+// tile rt's weights are free, for the loads that come next.
+template <int G, int RT, int CT, class F>
+__device__ __forceinline__ void block_product(const u4v (&w)[RT], const uint32_t (&p)[RT], const half8 (&x)[CT][4],
+                                              float4v (&acc)[RT][CT], F done) {
   constexpr int NG = 128 / G, J = G / 32;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane >> 4, col = lane & 15;
-  const int KB = (K + 127) >> 7, NT = (N + 15) >> 4;
-  const int T0 = blockIdx.x * RT;
-  const uint16_t* xp[CT];
+  // 8 in the codes' unit: its product with x is the sum of x that codes less 8
+  // lack, in all four rows of a lane.
+  const _Float16 e8 = (_Float16)(8.0f / kCodeUnit);
+  const half8 eights = {e8, e8, e8, e8, e8, e8, e8, e8};
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) xp[ct] = X + (int64_t)min(col + 16 * ct, B - 1) * ldx;
-  const u4v* wp[RT];
-  const u4v* pp[RT];
+  for (int g = 0; g < NG; ++g) {
+    float4v z[CT];
+    float xs[CT];
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int64_t T = min(T0 + rt, NT - 1);
-    wp[rt] = reinterpret_cast<const u4v*>(codes + T * KB * 1024) + lane;
-    pp[rt] = reinterpret_cast<const u4v*>(params + T * KB * NG * 32) + c;
-  }
-  const half8 ones = {(_Float16)1, (_Float16)1, (_Float16)1, (_Float16)1,
-                      (_Float16)1, (_Float16)1, (_Float16)1, (_Float16)1};
-  float4v acc[RT][CT];
+    for (int ct = 0; ct < CT; ++ct) {
+      z[ct] = float4v{0, 0, 0, 0};
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) acc[rt][ct] = float4v{0, 0, 0, 0};
-
-  typedef Block<G, RT, CT> Blk;
-  auto load = [&](Blk& d, int blk) {
+      for (int j = 0; j < J; ++j) z[ct] = mfma(eights, x[ct][g * J + j], z[ct]);
+      xs[ct] = z[ct][0] * 0.125f;   // the sum of x in the codes' unit
+    }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      d.w[rt] = wp[rt][(int64_t)blk * 64];
+      half8 a[J];
 #pragma unroll
-      for (int g = 0; g < NG; ++g) d.p[rt][g] = pp[rt][(int64_t)(blk * NG + g) * 4];
-    }
-    if (blk * 128 + 128 <= K) {
+      for (int j = 0; j < J; ++j) a[j] = code_operand(w[rt][g * J + j]);
+      half2v sm[4];
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d.x[ct][j] = load8(xp[ct] + blk * 128 + 32 * j + 8 * c);
-    } else {
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d.x[ct][j] = load_tail(xp[ct], blk * 128 + 32 * j + 8 * c, K);
-    }
-  };
-  auto compute = [&](const Blk& d) {
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float xs[CT];
+      for (int i = 0; i < 4; ++i) sm[i] = __builtin_bit_cast(half2v, row_bcast(p[rt], 4 * g + i));
+      if (g == NG - 1) done(rt);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        float4v t = {0, 0, 0, 0};
+        float4v t = z[ct];
 #pragma unroll
-        for (int j = 0; j < J; ++j) t = mfma(ones, d.x[ct][g * J + j], t);
-        xs[ct] = t[0];
-      }
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        half8 a[J];
-#pragma unroll
-        for (int j = 0; j < J; ++j) a[j] = code_operand(d.w[rt][g * J + j]);
-        float s[4], m[4];
+        for (int j = 0; j < J; ++j) t = mfma(a[j], x[ct][g * J + j], t);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          m[i] = centred(lo_half(d.p[rt][g][i]), hi_half(d.p[rt][g][i]));
-          s[i] = lo_half(d.p[rt][g][i]) * kCodeUnit;
-        }
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          float4v t = {0, 0, 0, 0};
-#pragma unroll
-          for (int j = 0; j < J; ++j) t = mfma(a[j], d.x[ct][g * J + j], t);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[rt][ct][i] = fmaf(s[i], t[i], fmaf(m[i], xs[ct], acc[rt][ct][i]));
+          acc[rt][ct][i] = fmaf((float)sm[i][0], t[i], acc[rt][ct][i]);
+          acc[rt][ct][i] = fmaf((float)sm[i][1], xs[ct], acc[rt][ct][i]);
         }
       }
     }
-  };
-
-  if constexpr (CT == 4) {   // four column tiles leave no registers for the next block
-    for (int blk = wave; blk < KB; blk += kWaves) {
-      Blk cur;
-      load(cur, blk);
-      compute(cur);
-    }
-  } else {
-  Blk cur, nxt;
-  if (wave < KB) load(cur, wave);
-  for (int blk = wave; blk < KB; blk += kWaves) {
-    const bool more = blk + kWaves < KB;
-    if (more) load(nxt, blk + kWaves);
-    compute(cur);
-    if (more) cur = nxt;
   }
-  }
+}
 
-  // The waves' sums, added in the waves' order.
-  __shared__ float4v part[kWaves][RT * CT][64];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) part[wave][rt * CT + ct][lane] = acc[rt][ct];
-  __syncthreads();
-  for (int i = threadIdx.x; i < RT * CT * 64; i += 64 * kWaves) {
+// The outputs of S sets of 16 rows (first row 16 T0) from the sums of W waves,
+// added in the waves' order; part[w][set * CT + ct][lane].
+template <int G, int S, int CT, int W>
+__device__ inline void write_outputs(const float4v (*part)[S * CT][64], const uint8_t* codes, const uint32_t* params,
+                                     const uint16_t* X, int64_t ldx, int T0, int N, int K, int B, void* Y,
+                                     int out_f32) {
+  for (int i = threadIdx.x; i < S * CT * 64; i += blockDim.x) {
     const int l = i & 63, ct = (i >> 6) % CT, rt = (i >> 6) / CT;
     const int b = 16 * ct + (l & 15);
     const int64_t n = (int64_t)(T0 + rt) * 16 + 4 * (l >> 4);
     if (b >= B || n >= N) continue;
     float4v y = part[0][rt * CT + ct][l];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) y += part[w][rt * CT + ct][l];
+    for (int k = 1; k < W; ++k) y += part[k][rt * CT + ct][l];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (n + e >= N) break;
       float v = y[e];
-      if (!(fabsf(v) < __builtin_inff())) v = by_weights(codes, params, K, KB, G, X + (int64_t)b * ldx, n + e);
+      if (!(fabsf(v) < __builtin_inff()))
+        v = by_weights(codes, params, K, (K + 127) >> 7, G, X + (int64_t)b * ldx, n + e);
       const int64_t at = (int64_t)b * N + n + e;
       if (out_f32)
         static_cast<float*>(Y)[at] = v;
@@ -267,26 +228,214 @@ __global__ void __launch_bounds__(64 * kWaves) q4_gemm_kernel(const uint8_t* __r
   }
 }
 
-template <int G, int RT, int CT>
-void start(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
+// Few rows of X: every wave reads the inputs of its block from memory in the
+// shape of the operand (16 bytes of up to four rows, 64 bytes apart from each
+// other's lanes).  A wave takes the blocks wave, wave + W, ... of RT row tiles,
+// NB of them in its registers or on their way.
+template <int G, int RT, int W, int NB>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) q4_gemv_kernel(const uint8_t* __restrict__ codes,
+                                                         const uint32_t* __restrict__ params,
+                                                         const uint16_t* __restrict__ X, int64_t ldx, int N, int K,
+                                                         int B, void* __restrict__ Y, int out_f32) {
+  constexpr int NG = 128 / G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane >> 4, col = lane & 15;
+  const int KB = (K + 127) >> 7, NT = (N + 15) >> 4;
+  const int T0 = blockIdx.x * RT;
+  const uint16_t* xp = X + (int64_t)min(col, B - 1) * ldx;
+  const u4v* wp[RT];
+  const uint32_t* pp[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int64_t T = min(T0 + rt, NT - 1);
+    wp[rt] = reinterpret_cast<const u4v*>(codes + T * KB * 1024) + lane;
+    pp[rt] = param_lane<NG>(params, T, KB);
+  }
+  float4v acc[RT][1];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) acc[rt][0] = float4v{0, 0, 0, 0};
+
+  u4v w[NB][RT];
+  uint32_t p[NB][RT];
+  half8 x[NB][1][4];
+  auto load_w = [&](int s, int rt, int blk) {
+    w[s][rt] = wp[rt][(int64_t)blk * 64];
+    p[s][rt] = pp[rt][(int64_t)blk * NG * 16];
+  };
+  auto load_x = [&](int s, int blk) {
+    if (blk * 128 + 128 <= K) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[s][0][j] = load8(xp + blk * 128 + 32 * j + 8 * c);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[s][0][j] = load_tail(xp, blk * 128 + 32 * j + 8 * c, K);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < NB; ++s) {
+    const int blk = min(wave + s * W, KB - 1);   // past the last block: read again, not used
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) load_w(s, rt, blk);
+    load_x(s, blk);
+  }
+  for (int blk0 = wave; blk0 < KB; blk0 += NB * W) {
+#pragma unroll
+    for (int s = 0; s < NB; ++s) {
+      if (blk0 + s * W >= KB) break;
+      const int next = min(blk0 + (NB + s) * W, KB - 1);
+      block_product<G, RT, 1>(w[s], p[s], x[s], acc, [&](int rt) { load_w(s, rt, next); });
+      load_x(s, next);
+    }
+  }
+  __shared__ float4v part[W][RT][64];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) part[wave][rt][lane] = acc[rt][0] * kCodeUnit;
+  __syncthreads();
+  write_outputs<G, RT, 1, W>(part, codes, params, X, ldx, T0, N, K, B, Y, out_f32);
+}
+
+// More rows of X: chunks of 128 WK inputs of all rows go through LDS, whole
+// lines of X from memory and operands from LDS, one chunk computed while the
+// next arrives.  Wave wr WK + wk takes block wk of a chunk and row tile wr of the
+// workgroup's WR.
+template <int G, int CT, int WK, int WR>
+__global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __restrict__ codes,
+                                                               const uint32_t* __restrict__ params,
+                                                               const uint16_t* __restrict__ X, int64_t ldx, int N,
+                                                               int K, int B, void* __restrict__ Y, int out_f32) {
+  constexpr int NG = 128 / G, KC = 128 * WK, kThreads = 64 * WK * WR, kRow = KC + 8;   // 16 bytes between rows: all banks
+  constexpr int kLoads = 16 * CT * (KC / 8) / kThreads;
+  extern __shared__ __align__(16) uint16_t lds[];   // [2][16 CT][kRow], then the waves' sums over it
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wk = wave % WK, wr = wave / WK;
+  const int c = lane >> 4, col = lane & 15;
+  const int KB = (K + 127) >> 7, NT = (N + 15) >> 4, chunks = (KB + WK - 1) / WK;
+  const int T0 = blockIdx.x * WR;
+  const int64_t T = min(T0 + wr, NT - 1);
+  const u4v* wp = reinterpret_cast<const u4v*>(codes + T * KB * 1024) + lane;
+  const uint32_t* pp = param_lane<NG>(params, T, KB);
+  float4v acc[1][CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) acc[0][ct] = float4v{0, 0, 0, 0};
+
+  // Thread i of the workgroup brings 8 inputs of kLoads rows, of two chunks in
+  // turn where the registers allow.
+  constexpr int kIn = kLoads <= 8 ? 2 : 1;
+  half8 in[kIn][kLoads];
+  auto fetch = [&](int s, int chunk) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = threadIdx.x + i * kThreads, row = at / (KC / 8), k = chunk * KC + at % (KC / 8) * 8;
+      const uint16_t* xr = X + (int64_t)min(row, B - 1) * ldx;
+      if (k + 8 <= K)
+        in[s][i] = load8(xr + k);
+      else
+        in[s][i] = load_tail(xr, k, K);
+    }
+  };
+  auto stage = [&](int s, int buf) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = threadIdx.x + i * kThreads, row = at / (KC / 8);
+      *reinterpret_cast<half8*>(&lds[(buf * 16 * CT + row) * kRow + at % (KC / 8) * 8]) = in[s][i];
+    }
+  };
+  u4v w[2][1];
+  uint32_t p[2][1];
+  auto load_w = [&](int s, int chunk) {
+    const int blk = min(chunk * WK + wk, KB - 1);
+    w[s][0] = wp[(int64_t)blk * 64];
+    p[s][0] = pp[(int64_t)blk * NG * 16];
+  };
+  load_w(0, 0);
+  fetch(0, 0);
+  if (kIn == 2 && chunks > 1) fetch(1, 1);
+  load_w(1, 1);
+  stage(0, 0);
+  __syncthreads();
+  for (int chunk0 = 0; chunk0 < chunks; chunk0 += 2) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int chunk = chunk0 + s;
+      if (chunk >= chunks) break;
+      const bool more = chunk + 1 < chunks;
+      if (chunk + kIn < chunks) fetch(kIn == 2 ? s : 0, chunk + kIn);
+      half8 x[CT][4];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[ct][j] = *reinterpret_cast<const half8*>(&lds[(s * 16 * CT + 16 * ct + col) * kRow + wk * 128 + 32 * j + 8 * c]);
+      // Blocks past the last one meet inputs of 0 only.
+      block_product<G, 1, CT>(w[s], p[s], x, acc, [&](int) { load_w(s, chunk + 2); });
+      if (more) stage(kIn == 2 ? s ^ 1 : 0, s ^ 1);
+      __syncthreads();
+    }
+  }
+  typedef float4v Part[WR * CT][64];
+  Part* part = reinterpret_cast<Part*>(lds);
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) part[wk][wr * CT + ct][lane] = acc[0][ct] * kCodeUnit;
+  __syncthreads();
+  write_outputs<G, WR, CT, WK>(part, codes, params, X, ldx, T0, N, K, B, Y, out_f32);
+}
+
+template <int G, int RT, int W, int NB>
+void start_gemv(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
   const int NT = (m.n_out + 15) / 16;
-  q4_gemm_kernel<G, RT, CT><<<(NT + RT - 1) / RT, 64 * kWaves, 0, s>>>(m.codes, m.params, X, ldx, m.n_out, m.n_in, B, Y,
-                                                                     out_f32 ? 1 : 0);
+  q4_gemv_kernel<G, RT, W, NB><<<(NT + RT - 1) / RT, 64 * W, 0, s>>>(
+      m.codes, reinterpret_cast<const uint32_t*>(m.params), X, ldx, m.n_out, m.n_in, B, Y, out_f32 ? 1 : 0);
+}
+
+template <int G, int CT, int WK, int WR>
+hipError_t start_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
+  const int NT = (m.n_out + 15) / 16;
+  constexpr int kStage = 2 * 16 * CT * (128 * WK + 8) * 2, kPart = WK * WR * CT * 64 * 16;
+  constexpr int kLds = kStage > kPart ? kStage : kPart;
+  static_assert(kLds <= 160 * 1024, "the LDS of a CU");
+  static std::atomic<bool> set[64];   // per device: the kernel's limit of LDS is raised
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= 64 || !set[dev].load(std::memory_order_relaxed)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_gemm_kernel<G, CT, WK, WR>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (e != hipSuccess) return e;
+    if (dev >= 0 && dev < 64) set[dev].store(true, std::memory_order_relaxed);
+  }
+  q4_gemm_kernel<G, CT, WK, WR><<<(NT + WR - 1) / WR, 64 * WK * WR, kLds, s>>>(
+      m.codes, reinterpret_cast<const uint32_t*>(m.params), X, ldx, m.n_out, m.n_in, B, Y, out_f32 ? 1 : 0);
+  return hipSuccess;
 }
 
 template <int G>
-void start_g(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
+hipError_t start_g(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
   const int NT = (m.n_out + 15) / 16;
-  if (B <= 16) {
+  // Up to 512 row tiles (two a CU) the waves of a workgroup divide K among
+  // them; beyond that they also take several row tiles, which share X.
+  //   B = 1, waves x row tiles, us: 4096 x 12288 8x1 8.8, 4x2 15; 12288 x 4096 8x1
+  //   11, 4x2 8.6, 4x4 10.4; 28000 x 4096 8x1 16, 4x2 13.3, 4x4 13.7; 131072 x 4096
+  //   4x2 65, 4x4 54, 8x4 65
+  //   B = 16, waves along K x row tiles: 4096 x 12288 16x1 11.2, 8x1 14, 4x4 21;
+  //   12288 x 4096 16x1 15, 4x4 10.2; 131072 x 4096 8x1 105, 8x2 96, 4x4 76
+  const bool wide = NT > 512;
+  if (B <= 2 || (B <= 4 && !wide)) {
     if (NT >= 2048)
-      start<G, G == 32 ? 2 : 4, 1>(m, X, ldx, B, Y, out_f32, s);
+      start_gemv<G, 4, 4, 1>(m, X, ldx, B, Y, out_f32, s);
+    else if (wide)
+      start_gemv<G, 2, 4, 1>(m, X, ldx, B, Y, out_f32, s);
     else
-      start<G, 1, 1>(m, X, ldx, B, Y, out_f32, s);
-  } else if (B <= 32) {
-    start<G, 1, 2>(m, X, ldx, B, Y, out_f32, s);
-  } else {
-    start<G, 1, 4>(m, X, ldx, B, Y, out_f32, s);
+      start_gemv<G, 1, 8, 1>(m, X, ldx, B, Y, out_f32, s);
+    return hipSuccess;
   }
+  if (B <= 16)
+    return wide ? start_gemm<G, 1, 4, 4>(m, X, ldx, B, Y, out_f32, s)
+                : start_gemm<G, 1, 16, 1>(m, X, ldx, B, Y, out_f32, s);
+  if (B <= 32)
+    return wide ? start_gemm<G, 2, 4, 4>(m, X, ldx, B, Y, out_f32, s)
+                : start_gemm<G, 2, 8, 1>(m, X, ldx, B, Y, out_f32, s);
+  return wide ? start_gemm<G, 4, 2, 4>(m, X, ldx, B, Y, out_f32, s)
+              : start_gemm<G, 4, 4, 2>(m, X, ldx, B, Y, out_f32, s);
 }
 
 }  // namespace
@@ -310,13 +459,10 @@ hipError_t launch_q4_unpack(const Q4Dev& m, uint16_t* w, hipStream_t s) {
 
 hipError_t launch_q4_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32,
                           hipStream_t s) {
-  if (m.group == 32)
-    start_g<32>(m, X, ldx, B, Y, out_f32, s);
-  else if (m.group == 64)
-    start_g<64>(m, X, ldx, B, Y, out_f32, s);
-  else
-    start_g<128>(m, X, ldx, B, Y, out_f32, s);
-  return hipGetLastError();
+  const hipError_t e = m.group == 32   ? start_g<32>(m, X, ldx, B, Y, out_f32, s)
+                       : m.group == 64 ? start_g<64>(m, X, ldx, B, Y, out_f32, s)
+                                       : start_g<128>(m, X, ldx, B, Y, out_f32, s);
+  return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace tq

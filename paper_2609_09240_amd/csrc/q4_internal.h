@@ -107,6 +107,18 @@ __device__ inline half8 code_operand(uint32_t w) {
   const half2v r3 = __builtin_elementwise_fma(__builtin_bit_cast(half2v, t & 0x00F000F0u), b, m);
   return half8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
 }
+// Lane n of each 16 to all of them (n a constant).
+#define TQ_ROW_BCAST(n) case n: return __builtin_amdgcn_update_dpp(0, x, 0x150 + n, 0xF, 0xF, false);
+__device__ __forceinline__ uint32_t row_bcast(uint32_t x, int n) {
+  switch (n) {
+    TQ_ROW_BCAST(0) TQ_ROW_BCAST(1) TQ_ROW_BCAST(2) TQ_ROW_BCAST(3) TQ_ROW_BCAST(4) TQ_ROW_BCAST(5)
+    TQ_ROW_BCAST(6) TQ_ROW_BCAST(7) TQ_ROW_BCAST(8) TQ_ROW_BCAST(9) TQ_ROW_BCAST(10) TQ_ROW_BCAST(11)
+    TQ_ROW_BCAST(12) TQ_ROW_BCAST(13) TQ_ROW_BCAST(14)
+    default: return __builtin_amdgcn_update_dpp(0, x, 0x15F, 0xF, 0xF, false);
+  }
+}
+#undef TQ_ROW_BCAST
+
 // The offset that goes with codes around 0.
 __device__ inline float centred(float s, float m) { return fmaf(8.0f, s, m); }
 
