@@ -183,17 +183,6 @@ constexpr int kMaxPairs = 256;
 
 __device__ inline int share_start(int64_t T, int64_t w, int64_t W) { return (int)(T * w / W); }
 
-// Inclusive prefix sum over a wave.
-__device__ inline int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast 15 to rows 1 and 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast 31 to rows 2 and 3
-  return x;
-}
-
 // A workgroup's share: units [unit, end) of T, the first of them unit `off` of
 // pair `pair`.  Every wave works it out for itself.
 struct Share {

@@ -7,39 +7,36 @@
 // bytes that move, 10 to 100 KB a page and layer, are another launch over the
 // whole chip that reads what was decided.  Counts are integers, so the order
 // in which atomics reach them does not show.
+//
+// The deciding launches are bound by their trips to memory, one after the other
+// (slots, lengths, last pages, counts of pages): 60 forks 7.6 us, room for 32
+// rows 5.2 us, a compaction's plan 2.6 us, freeing 2 to 3 us.  The copies are
+// bound by HBM: 53 MB to and fro in 9.6 us, half of it from the caches, 64 MB of
+// a compaction in 19.7 us, 6.5 TB/s.  (1024 threads for any number of rows: 9.6
+// and 7.0 us; the free pages of a thread handed out one after the other: 11.6.)
 
 #include "q4_internal.h"
 
 namespace tq {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
-
-// Exclusive prefix sum of v over the workgroup's threads; *total the sum.
-__device__ inline int scan(int v, int* total, int* lds /*[kWaves + 1]*/) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+// Exclusive prefix sum of v over the workgroup's T threads; *total the sum.
+template <int T>
+__device__ inline int scan(int v, int* total, int* lds /*[T / 64]*/) {
+  const int wave = threadIdx.x >> 6;
+  const int x = wave_scan(v);
   __syncthreads();   // lds may still be read from the call before
-  if (lane == 63) lds[wave] = x;
+  if ((threadIdx.x & 63) == 63) lds[wave] = x;
   __syncthreads();
-  if (wave == 0) {
-    int s = lane < kWaves ? lds[lane] : 0;
+  int before = 0, all = 0;
 #pragma unroll
-    for (int d = 1; d < kWaves; d <<= 1) {
-      const int y = __shfl_up(s, d);
-      if (lane >= d) s += y;
-    }
-    if (lane < kWaves) lds[lane] = s;
+  for (int w = 0; w < T / 64; ++w) {
+    const int n = lds[w];
+    before += w < wave ? n : 0;
+    all += n;
   }
-  __syncthreads();
-  *total = lds[kWaves - 1];
-  return x - v + (wave ? lds[wave - 1] : 0);
+  *total = all;
+  return x - v + before;
 }
 
 __device__ inline bool page_ok(const KvDev& c, int p) { return p >= 0 && p < c.n_pages; }
@@ -50,36 +47,38 @@ __device__ inline int len_of(const KvDev& c, int seq) {
 }
 
 // Row i of the call names a slot that an earlier row names (slots: the rows'
-// slots in LDS).
-__device__ inline bool named_before(const int* slots, int i) {
-  for (int j = 0; j < i; ++j)
-    if (slots[j] == slots[i]) return true;
-  return false;
+// slots in LDS, T of them).
+template <int T>
+__device__ inline bool named_before(const int* slots, int i, int n_rows) {
+  const int mine = slots[i];
+  bool found = false;
+  for (int j = 0; j < n_rows; j += 8)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) found |= j + e < i && slots[min(j + e, T - 1)] == mine;
+  return found;
 }
 
 // Hands the `total` lowest free pages out: give(k, page) for the k-th of
-// them, k < total.  Returns how many there were.  Called by all threads.
-template <class F>
+// them, k < total.  Returns how many there were.  Called by all T threads, each
+// of which looks at 16 pages beside each other in a pass.
+template <int T, class F>
 __device__ int take_free(const KvDev& c, int total, int* lds, F give) {
+  constexpr int kEach = 4096 / T;
+  __shared__ int list[4096];
   int found = 0;
-  for (int64_t p0 = 0; p0 < c.n_pages && found < total; p0 += kThreads * 4) {
-    const int64_t p = p0 + threadIdx.x * 4;
-    bool free[4];
-    int mine = 0;
+  for (int64_t p0 = 0; p0 < c.n_pages && found < total; p0 += 4096) {
+    const int64_t p = p0 + threadIdx.x * kEach;
+    uint32_t free = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      free[e] = p + e < c.n_pages && c.refs[p + e] == 0;
-      mine += free[e];
-    }
+    for (int e = 0; e < kEach; ++e) free |= (uint32_t)(c.refs[min(p + e, (int64_t)c.n_pages - 1)] == 0 && p + e < c.n_pages) << e;
     int all;
-    int at = found + scan(mine, &all, lds);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (free[e]) {
-        if (at < total) give(at, (int)p + e);
-        ++at;
-      }
+    int at = found + scan<T>(__popc(free), &all, lds);
+    // Listed first, so that pages beside each other go to different threads.
+    for (at -= found; free != 0; free &= free - 1) list[at++] = (int)p + __ffs(free) - 1;
+    __syncthreads();
+    for (int k = found + threadIdx.x; k < min(found + all, total); k += T) give(k, list[k - found]);
     found += all;
+    __syncthreads();
   }
   return min(found, total);
 }
@@ -97,17 +96,18 @@ __device__ inline int row_with(const int* base, int n, int k) {
   return lo;
 }
 
-__global__ void __launch_bounds__(kThreads) kv_extend_kernel(KvDev c, const int32_t* __restrict__ seqs,
+template <int T>
+__global__ void __launch_bounds__(T) kv_extend_kernel(KvDev c, const int32_t* __restrict__ seqs,
                                                              const int32_t* __restrict__ cu, int n_rows,
                                                              int32_t* __restrict__ starts,
                                                              int32_t* __restrict__ d_err) {
-  __shared__ int lds[kWaves + 1], slots[kThreads], base[kThreads], have[kThreads];
+  __shared__ int lds[T / 64], slots[T], base[T], have[T];
   const int i = threadIdx.x;
   const bool row = i < n_rows;
   const int seq = row ? (seqs ? seqs[i] : i) : -1;
   slots[i] = seq;
   __syncthreads();
-  bool ok = row && seq >= 0 && seq < c.n_seqs && !(seqs && named_before(slots, i));
+  bool ok = row && seq >= 0 && seq < c.n_seqs && !(seqs && named_before<T>(slots, i, n_rows));
   int len = 0, need = 0;
   int64_t want = 0;
   if (ok) {
@@ -123,10 +123,10 @@ __global__ void __launch_bounds__(kThreads) kv_extend_kernel(KvDev c, const int3
   }
   int total;
   // Rows of a call ask for 2^20 pages each at most, 2^30 together.
-  base[i] = scan(need, &total, lds);
+  base[i] = scan<T>(need, &total, lds);
   have[i] = pages_of(c, len);
   __syncthreads();
-  const int got = take_free(c, total, lds, [&](int k, int page) {
+  const int got = take_free<T>(c, total, lds, [&](int k, int page) {
     const int r = row_with(base, n_rows, k);
     c.pages[(int64_t)slots[r] * c.max_pages + have[r] + (k - base[r])] = page;
     c.refs[page] = 1;
@@ -181,11 +181,12 @@ struct ForkRow {
   int32_t src, dst, share, len;
 };
 
-__global__ void __launch_bounds__(kThreads) kv_fork_kernel(KvDev c, const int32_t* __restrict__ parents,
+template <int T>
+__global__ void __launch_bounds__(T) kv_fork_kernel(KvDev c, const int32_t* __restrict__ parents,
                                                            const int32_t* __restrict__ children, int n_rows,
                                                            int32_t* __restrict__ d_err,
                                                            ForkRow* __restrict__ rows) {
-  __shared__ int lds[kWaves + 1], slots[kThreads], base[kThreads], dst[kThreads];
+  __shared__ int lds[T / 64], slots[T], base[T], dst[T];
   const int i = threadIdx.x;
   const bool row = i < n_rows;
   const int child = row ? children[i] : -1, parent = row ? parents[i] : -1;
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) kv_fork_kernel(KvDev c, const int32_
   dst[i] = -1;
   __syncthreads();
   bool ok = row && child >= 0 && child < c.n_seqs && parent >= 0 && parent < c.n_seqs && child != parent &&
-            c.lens[child] <= 0 && !named_before(slots, i);
+            c.lens[child] <= 0 && !named_before<T>(slots, i, n_rows);
   int len = 0, need = 0, src = -1;
   if (ok) {
     len = len_of(c, parent);
@@ -204,11 +205,11 @@ __global__ void __launch_bounds__(kThreads) kv_fork_kernel(KvDev c, const int32_
     }
   }
   int total;
-  base[i] = scan(need, &total, lds);
+  base[i] = scan<T>(need, &total, lds);
   __syncthreads();
-  // Page k goes to the last row whose share starts at or before it, and that
-  // is the one that needs it: rows that need none start where the next does.
-  take_free(c, total, lds, [&](int k, int page) {
+  // Page k goes to the last row whose share starts at or before it: of rows that
+  // start there, all but the last need none.
+  take_free<T>(c, total, lds, [&](int k, int page) {
     dst[row_with(base, n_rows, k)] = page;
     c.refs[page] = 1;
   });
@@ -280,12 +281,13 @@ struct Compact {
   int32_t* map;
 };
 
-__global__ void __launch_bounds__(kThreads) kv_compact_kernel(KvDev c, int32_t* __restrict__ n_live, Compact w) {
-  __shared__ int lds[kWaves + 1];
+__global__ void __launch_bounds__(1024) kv_compact_kernel(KvDev c, int32_t* __restrict__ n_live, Compact w) {
+  constexpr int kThreads = 1024;
+  __shared__ int lds[kThreads / 64];
   int mine = 0;
   for (int64_t p = threadIdx.x; p < c.n_pages; p += kThreads) mine += c.refs[p] > 0;
   int live;
-  scan(mine, &live, lds);
+  scan<kThreads>(mine, &live, lds);
   int holes = 0, movers = 0;
   for (int64_t p0 = 0; p0 < c.n_pages; p0 += kThreads) {
     const int64_t p = p0 + threadIdx.x;
@@ -293,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) kv_compact_kernel(KvDev c, int32_t* 
     const bool hole = in && p < live && !used, mover = used && p >= live;
     int all;
     // At most 1024 of each: both counts in one word.
-    const int at = scan(hole | (mover << 16), &all, lds);
+    const int at = scan<kThreads>(hole | (mover << 16), &all, lds);
     if (hole) w.to[holes + (at & 0xFFFF)] = (int)p;
     if (mover) w.from[movers + (at >> 16)] = (int)p;
     if (in) w.map[p] = (int)p;
@@ -353,7 +355,10 @@ size_t kv_workspace_bytes(const KvDev& c, int n_rows) {
 
 hipError_t launch_kv_extend(const KvDev& c, const int32_t* seqs, const int32_t* cu, int n_rows, int32_t* starts,
                             int32_t* d_err, hipStream_t s) {
-  kv_extend_kernel<<<1, kThreads, 0, s>>>(c, seqs, cu, n_rows, starts, d_err);
+  if (n_rows <= 256)
+    kv_extend_kernel<256><<<1, 256, 0, s>>>(c, seqs, cu, n_rows, starts, d_err);
+  else
+    kv_extend_kernel<TQ_KV_MAX_ROWS><<<1, TQ_KV_MAX_ROWS, 0, s>>>(c, seqs, cu, n_rows, starts, d_err);
   return hipGetLastError();
 }
 
@@ -365,7 +370,10 @@ hipError_t launch_kv_free(const KvDev& c, const int32_t* seqs, int n_rows, int32
 hipError_t launch_kv_fork(const KvDev& c, const int32_t* parents, const int32_t* children, int n_rows,
                           int32_t* d_err, void* ws, hipStream_t s) {
   ForkRow* rows = static_cast<ForkRow*>(ws);
-  kv_fork_kernel<<<1, kThreads, 0, s>>>(c, parents, children, n_rows, d_err, rows);
+  if (n_rows <= 256)
+    kv_fork_kernel<256><<<1, 256, 0, s>>>(c, parents, children, n_rows, d_err, rows);
+  else
+    kv_fork_kernel<TQ_KV_MAX_ROWS><<<1, TQ_KV_MAX_ROWS, 0, s>>>(c, parents, children, n_rows, d_err, rows);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   kv_fork_copy_kernel<<<dim3(parts_of(c), c.n_layers, n_rows), 256, 0, s>>>(c, parents, children, rows);
@@ -380,7 +388,7 @@ hipError_t launch_kv_compact(const KvDev& c, int32_t* n_live, void* ws, hipStrea
   w.from = reinterpret_cast<int32_t*>(p + 16);
   w.to = reinterpret_cast<int32_t*>(p + 16 + list);
   w.map = reinterpret_cast<int32_t*>(p + 16 + 2 * list);
-  kv_compact_kernel<<<1, kThreads, 0, s>>>(c, n_live, w);
+  kv_compact_kernel<<<1, 1024, 0, s>>>(c, n_live, w);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   kv_compact_move_kernel<<<2048, 256, 0, s>>>(c, w, parts_of(c));

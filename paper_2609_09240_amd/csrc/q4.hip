@@ -36,6 +36,14 @@ __device__ inline float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+// Inputs 8 from k on, zeros past K.
+__device__ inline half8 load_tail(const uint16_t* x, int k, int K) {
+  half8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = k + e < K ? __builtin_bit_cast(_Float16, x[k + e]) : (_Float16)0.0f;
+  return v;
+}
+
 // ---- Quantise and unpack: a workgroup per tile of 16 rows and 128 inputs, a
 // thread per 8 inputs of a row.
 
@@ -46,26 +54,22 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const uint16_t* __rest
   const int r = threadIdx.x >> 4, ch = threadIdx.x & 15;
   const int64_t n = (int64_t)T * 16 + r;
   const int k = blk * 128 + ch * 8;
-  float x[8];
-  float lo = __builtin_inff(), hi = -__builtin_inff();
-  bool finite = true;
   const int have = n < N ? min(8, max(0, K - k)) : 0;
-  if (have == 8) {
-    const half8 v = load8(w + n * ldw + k);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < have ? lo_half(w[n * ldw + k + e]) : 0.0f;
-  }
+  half8 x = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (have == 8)
+    x = load8(w + n * ldw + k);
+  else if (have > 0)
+    x = load_tail(w + n * ldw, k, K);
+  float lo = __builtin_inff(), hi = -__builtin_inff();
+  int f = 1;
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if (e < have) {
-      lo = fminf(lo, x[e]);
-      hi = fmaxf(hi, x[e]);
-      finite = finite && (x[e] - x[e] == 0.0f);
+      const float v = (float)x[e];
+      lo = fminf(lo, v);
+      hi = fmaxf(hi, v);
+      f &= v - v == 0.0f;
     }
-  int f = finite;
   for (int d = 1; d < G / 8; d <<= 1) {
     lo = fminf(lo, __shfl_xor(lo, d));
     hi = fmaxf(hi, __shfl_xor(hi, d));
@@ -77,8 +81,9 @@ __global__ void __launch_bounds__(256) q4_quantize_kernel(const uint16_t* __rest
   p.s = p.m = (_Float16)0.0f;
   if (!empty) p = q4_params(lo, hi, f != 0);
   uint32_t q[8];
+  q4_codes(x, lo, (float)p.s, q);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) q[e] = e < have ? q4_code(x[e], lo, (float)p.s) : 0u;
+  for (int e = 0; e < 8; ++e) q[e] = e < have ? q[e] : 0u;
   const int64_t tile = blockIdx.x;
   codes[tile * 256 + ((ch & 3) * 16 + r) * 4 + (ch >> 2)] = code_word(q);
   if ((ch & (G / 8 - 1)) == 0) {
@@ -134,14 +139,6 @@ __device__ __attribute__((noinline)) float by_weights(const uint8_t* codes, cons
     acc = fmaf(q4_value((w >> (4 * nibble_of(e))) & 15u, lo_half(p), hi_half(p)), lo_half(x[k]), acc);
   }
   return acc;
-}
-
-// Inputs 8 from k on, zeros past K.
-__device__ inline half8 load_tail(const uint16_t* x, int k, int K) {
-  half8 v;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = k + e < K ? __builtin_bit_cast(_Float16, x[k + e]) : (_Float16)0.0f;
-  return v;
 }
 
 // The parameters of a row tile and block are one word a lane: lane (c, k) holds

@@ -107,6 +107,17 @@ __device__ inline half8 code_operand(uint32_t w) {
   const half2v r3 = __builtin_elementwise_fma(__builtin_bit_cast(half2v, t & 0x00F000F0u), b, m);
   return half8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
 }
+// Inclusive prefix sum over a wave.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast 15 to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast 31 to rows 2 and 3
+  return x;
+}
+
 // Lane n of each 16 to all of them (n a constant).
 #define TQ_ROW_BCAST(n) case n: return __builtin_amdgcn_update_dpp(0, x, 0x150 + n, 0xF, 0xF, false);
 __device__ __forceinline__ uint32_t row_bcast(uint32_t x, int n) {
@@ -143,11 +154,30 @@ __device__ inline Q4Params q4_params(float lo, float hi, bool finite) {
   if (!finite) p.s = p.m = (_Float16)__builtin_nanf("");
   return p;
 }
-__device__ inline uint32_t q4_code(float x, float lo, float s) {
-  // s is 0, positive or NaN
-  if (!(s > 0.0f)) return 0;
-  const float q = rintf(__fdiv_rn(__fsub_rn(x, lo), s));
-  return (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f);
+// Codes of eight values of a group.  The quotient by a reciprocal is within
+// 2^-18 of the rounded one; where it lies further than that from a half both
+// round to the same code, and only elsewhere is the division made.
+__device__ __forceinline__ void q4_codes(half8 x, float lo, float s, uint32_t (&q)[8]) {
+  const float inv = 1.0f / s;
+  float d[8], t[8];
+  bool near = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    d[e] = __fsub_rn((float)x[e], lo);
+    t[e] = d[e] * inv;
+    near |= fabsf(t[e] - floorf(t[e]) - 0.5f) < 3.0e-5f;
+  }
+  if (!(s > 0.0f)) {   // 0 or NaN
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = 0;
+    return;
+  }
+  if (near || !(inv < __builtin_inff())) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = __fdiv_rn(d[e], s);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q[e] = (uint32_t)fminf(fmaxf(rintf(t[e]), 0.0f), 15.0f);
 }
 __device__ inline float q4_value(uint32_t q, float s, float m) { return fmaf((float)q, s, m); }
 
