@@ -377,6 +377,7 @@ tq_status tq_gemv_chain(const void* plan, void* sync, const tq_chain_info* info,
 #define TQ_Q4_MAX_IN (1 << 20)
 #define TQ_KV_MAX_ROWS 1024     /* rows of a call that changes the page table */
 #define TQ_KV_MAX_PAGES (1 << 20)   /* pages of one sequence */
+#define TQ_KV_MAX_HEADS 65520       /* query heads in tq_kv_attention */
 
 /* Non-owning view of a matrix of 4-bit weights.  N and K may be any sizes;
  * the last tile of rows and the last 128 inputs are filled up with codes and
@@ -410,16 +411,26 @@ tq_status tq_q4_quantize(const uint16_t* w, int64_t ldw, const tq_q4_matrix* m,
  * rounding), then rounded to fp16.  w is 2-byte aligned. */
 tq_status tq_q4_unpack_fp16(const tq_q4_matrix* m, uint16_t* w, void* stream);
 
+/* Bytes of workspace with which tq_q4_gemm is fastest (host function). */
+size_t tq_q4_workspace_bytes(const tq_q4_matrix* m, int32_t B);
+
 /* Y = X W^T for B = 1..TQ_Q4_MAX_BATCH rows of fp16 activations.
  *   X  fp16, rows ldx >= K elements apart; 2-byte aligned
  *   Y  [B][N], fp16 (TQ_OUT_FP16) or fp32 (TQ_OUT_FP32); 4-byte aligned
+ *   workspace  NULL, or tq_q4_workspace_bytes of the same arguments (0 for
+ *      most), 16-byte aligned: with it K is split among workgroups where more
+ *      than 16 rows meet few outputs.  It holds counts that every call finds
+ *      and leaves 0: it is filled with zeros once, before its first call, and
+ *      serves any calls that do not overlap in time.
  * scale * sum(code * x) + offset * sum(x) per group, every product exact,
- * sums in fp32; a row's result depends on the row and on which of 1..16,
- * 17..32, 33..64 B lies in, not on the other rows.  Where that is not finite
+ * sums in fp32; a row's result depends on the row, on the range of B (1 or 2,
+ * 3 or 4, 5..16, 17..32, 33..64) and on whether there is a workspace, not on
+ * the other rows.  Where that is not finite
  * the output is the fp32 sum of x times the weights formed one by one, so an
  * infinite input under a weight that is not 0 gives an infinity. */
 tq_status tq_q4_gemm(const tq_q4_matrix* m, const uint16_t* X, int64_t ldx,
-                     int32_t B, void* Y, int32_t flags, void* stream);
+                     int32_t B, void* Y, int32_t flags, void* workspace,
+                     size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Key/value cache held in 4 bits, in pages.
@@ -564,7 +575,8 @@ typedef struct tq_kv_attn {
   int32_t n_rows;           /* >= 1 */
   int32_t n_tokens;         /* tokens of q and o, >= 1 */
   int32_t max_q;            /* queries of a row, >= 1 */
-  int32_t n_heads;          /* a multiple of n_kv_heads */
+  int32_t n_heads;          /* a multiple of n_kv_heads, up to TQ_KV_MAX_HEADS;
+                               n_tokens * n_heads < 2^31 */
   int32_t max_len;
   int32_t window;           /* 0: none */
   float scale;

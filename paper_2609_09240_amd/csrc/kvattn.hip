@@ -28,12 +28,12 @@
 // SIMD.  One token over one long cache: 5.4 TB/s for every further byte, and
 // 6 us of launch, table, first loads and joining waves before the first, 7 us
 // for joining 96 parts a head.
-//   1 x 131072 tokens, 8 heads, groups of 128 (143 MB)  39.7 us
-//   32 ragged rows to 8192, groups of 64 (93 MB)        34.0
-//   1 x 4096 (4.7 MB)                                   11.9
-//   1 x 45                                              6.4
+//   1 x 131072 tokens, 8 heads, groups of 128 (143 MB)  39.3 us
+//   32 ragged rows to 8192, groups of 64 (93 MB)        32.2
+//   1 x 4096 (4.7 MB)                                   11.8
+//   1 x 45                                              6.5
 //   a chunk of 2 x 1000 queries over up to 5000, window 2048, 14 heads of 64 on
-//   2, groups of 32 (10 GFLOP)                          77
+//   2, groups of 32 (10 GFLOP)                          68
 // (One launch a split and another to join: 31 + 6.5, 33 + 6 and 10 + 6 for the
 // first three, and 3 us between the launches.  32 or 64 rows a tile, which
 // unpack a record once for two or four tiles, halve the waves: 90 and 120 us
@@ -103,6 +103,7 @@ struct Args {
   int64_t q_ts, q_hs, page_bytes;
   float scale_log2;
   int32_t n_rows, n_tokens, max_q, H, share, window;
+  uint32_t share_magic;    // floor(2^32 / share) + 1
   int32_t page_shift, n_seqs, max_pages, n_pages;
   int32_t tiles;           // tiles of a row
   int32_t shares;          // workgroups that divide the work evenly; 0: one per tile and head
@@ -116,44 +117,53 @@ struct Tile {
   int seq, first, n, rows;   // slot, first token in q, tokens, rows of (b, h) in all
   int64_t asked;             // tokens the call names for the row, max_q or not
   int len;
-  int row0;                  // first of the tile's rows
+  int row0, tok0, head0;     // first of the tile's rows, its token and head
   int rec0, rec1;            // records it can see
   int units;                 // of four records, one a wave; 1 where there are none
 };
 
-__device__ inline bool tile_of(const Args& a, int id, Tile* t) {
-  t->h = id % a.H;
-  t->b = id / a.H % a.n_rows;
-  t->qt = id / a.H / a.n_rows;
-  t->seq = a.seqs ? as_table(a.seqs)[t->b] : t->b;
-  int64_t first = a.cu ? as_table(a.cu)[t->b] : t->b, end = a.cu ? as_table(a.cu)[t->b + 1] : (int64_t)t->b + 1;
+// x / share for x < share + 16 <= 2^16.
+__device__ inline int by_share(const Args& a, int x) {
+  return a.share == 1 ? x : (int)__umulhi((uint32_t)x, a.share_magic);
+}
+
+// Tile (b, qt) of head 0; false where there is none.
+__device__ inline bool tile_of(const Args& a, int b, int qt, Tile* t) {
+  t->h = 0;
+  t->b = b;
+  t->qt = qt;
+  t->seq = a.seqs ? as_table(a.seqs)[b] : b;
+  int64_t first = a.cu ? as_table(a.cu)[b] : b, end = a.cu ? as_table(a.cu)[b + 1] : (int64_t)b + 1;
   const int64_t asked = t->asked = end - first;
   const bool bad = first < 0 || asked < 0;
   end = min(min(end, (int64_t)a.n_tokens), first + a.max_q);
   t->first = (int)first;
   t->n = bad || end <= first ? 0 : (int)(end - first);
   t->rows = t->n * a.share;
-  t->row0 = t->qt * 16;
+  t->row0 = qt * 16;
   if (t->row0 >= t->rows) return false;
+  t->tok0 = qt == 0 ? 0 : t->row0 / a.share;
+  t->head0 = t->row0 - t->tok0 * a.share;
   t->len = 0;
   if (t->seq >= 0 && t->seq < a.n_seqs)
     t->len = (int)min(min(max((int64_t)as_table(a.lens)[t->seq], (int64_t)0), (int64_t)a.max_pages << a.page_shift),
                       (int64_t)INT32_MAX - 64);
   // Position of query token i is base + i; all of what was asked for counts.
   const int64_t base = t->len - asked;
-  const int i0 = t->row0 / a.share, i1 = min(t->row0 + 16 - 1, t->rows - 1) / a.share;
-  const int64_t hi = min((int64_t)t->len, base + i1 + 1);
-  const int64_t lo = a.window > 0 ? max((int64_t)0, base + i0 + 1 - a.window) : 0;
+  const int last = min(t->tok0 + by_share(a, t->head0 + 15), t->n - 1);
+  const int64_t hi = min((int64_t)t->len, base + last + 1);
+  const int64_t lo = a.window > 0 ? max((int64_t)0, base + t->tok0 + 1 - a.window) : 0;
   t->rec0 = (int)(lo >> 5);
   t->rec1 = hi > lo ? (int)((hi + 31) >> 5) : t->rec0;
   t->units = max(1, (t->rec1 - t->rec0 + kWaves - 1) / kWaves);
   return true;
 }
 
-// o and lse of one row: four channels of the joined sum y, what it is divided
-// by, the reference.
-__device__ inline void store_row(const Args& a, const Tile& t, int D, int row, int d, float4v y, float sum, float ref) {
-  const int64_t at = (int64_t)(t.first + row / a.share) * (a.H * a.share) + t.h * a.share + row % a.share;
+// o and lse of row r of a tile: four channels of the joined sum y, what it is
+// divided by, the reference.
+__device__ inline void store_row(const Args& a, const Tile& t, int D, int r, int d, float4v y, float sum, float ref) {
+  const int tok = by_share(a, t.head0 + r), head = t.head0 + r - tok * a.share;
+  const int64_t at = (int64_t)(t.first + t.tok0 + tok) * (a.H * a.share) + t.h * a.share + head;
   y *= sum == 0.0f ? 0.0f : 1.0f / sum;
   if (a.out_f32) {
     *reinterpret_cast<float4v*>(static_cast<float*>(a.o) + at * D + d) = y;
@@ -164,30 +174,23 @@ __device__ inline void store_row(const Args& a, const Tile& t, int D, int row, i
   if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -__builtin_inff() : (ref + log2f(sum)) * kLn2;
 }
 
-// What crosses workgroups is stored and loaded at device scope, past the
-// caches of a die (sc1), so that no cache has to be written back or
-// invalidated: fences before and after the count cost 200 us a call, these 2.
-constexpr int kCoherent = 16;
-__device__ inline void put4(__amdgpu_buffer_rsrc_t r, int at, float4v v) {
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, v), r, at, 0, kCoherent);
-}
-__device__ inline float4v get4(__amdgpu_buffer_rsrc_t r, int at) {
-  return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kCoherent));
-}
-
 // Even shares: the units of all tiles and heads in a line (tiles by qt, then
-// row, then head), of which workgroup w of W takes [T w / W, T (w + 1) / W).
-// A pair is a tile and row, qt * n_rows + row; up to 256 of them, up to four
-// beside each other in a lane.
+// row, then head), which W workgroups divide: the first T % W take one more than
+// the others.  A pair is a tile and row, qt * n_rows + row; up to 256 of them, up
+// to four beside each other in a lane.
 constexpr int kMaxPairs = 256;
-
-__device__ inline int share_start(int64_t T, int64_t w, int64_t W) { return (int)(T * w / W); }
 
 // A workgroup's share: units [unit, end) of T, the first of them unit `off` of
 // pair `pair`.  Every wave works it out for itself.
 struct Share {
-  int T, W, unit, end, pair, off;
+  int q, more;             // units of every share, and how many shares have one more
+  int unit, end, pair, off;
 };
+__device__ inline int share_start(const Share& s, int w) { return w * s.q + min(w, s.more); }
+__device__ inline int share_with(const Share& s, int unit) {
+  const int head = s.more * (s.q + 1);
+  return unit < head ? unit / (s.q + 1) : s.more + (unit - head) / s.q;
+}
 __device__ inline Share share_of(const Args& a) {
   const int lane = threadIdx.x & 63, pairs = a.n_rows * a.tiles, per = (pairs + 63) >> 6;
   int n[kMaxPairs / 64], sum = 0;
@@ -197,18 +200,20 @@ __device__ inline Share share_of(const Args& a) {
     n[e] = 0;
     if (e < per && i < pairs) {
       Tile t;
-      if (tile_of(a, i * a.H, &t)) n[e] = t.units * a.H;
+      const int qt = a.tiles == 1 ? 0 : i / a.n_rows;
+      if (tile_of(a, i - qt * a.n_rows, qt, &t)) n[e] = t.units * a.H;
     }
     sum += n[e];
   }
   const int incl = wave_scan(sum);
   Share s;
-  s.T = __builtin_amdgcn_readlane(incl, 63);
-  s.W = min(a.shares, s.T);
-  s.unit = s.end = s.pair = s.off = 0;
-  if ((int)blockIdx.x >= s.W) return s;
-  s.unit = share_start(s.T, blockIdx.x, s.W);
-  s.end = share_start(s.T, blockIdx.x + 1, s.W);
+  const int T = __builtin_amdgcn_readlane(incl, 63), W = min(a.shares, T);
+  s.q = s.more = s.unit = s.end = s.pair = s.off = 0;
+  if ((int)blockIdx.x >= W) return s;
+  s.q = T / W;
+  s.more = T - s.q * W;
+  s.unit = share_start(s, blockIdx.x);
+  s.end = share_start(s, blockIdx.x + 1);
   // The last lane, then pair, that starts at or before the unit.
   const int at = __popcll(__builtin_amdgcn_ballot_w64(incl - sum <= s.unit)) - 1;
   s.pair = at * per;
@@ -257,7 +262,7 @@ kv_attn_kernel(Args args) {
   __shared__ float sm[kWaves][16], sl[kWaves][16];
   __shared__ float so[kWaves][16][D + 4];
   __shared__ int arrived;
-  Share share = {1, 1, 0, 1, 0, 0};
+  Share share = {1, 0, 0, 1, 0, 0};
   if (args.shares > 0) share = share_of(args);
   const int first_unit = share.unit;
   Tile t;
@@ -271,7 +276,10 @@ kv_attn_kernel(Args args) {
   const int slot = 2 * blockIdx.x + (share.unit != first_unit);
   if (a.shares > 0) {
     if (fresh) {
-      while (!tile_of(a, share.pair * a.H, &t)) ++share.pair;   // there is one: units are left
+      for (;; ++share.pair) {   // there is one: units are left
+        const int qt = a.tiles == 1 ? 0 : share.pair / a.n_rows;
+        if (tile_of(a, share.pair - qt * a.n_rows, qt, &t)) break;
+      }
       h = share.off / t.units;
       share.off -= h * t.units;
     }
@@ -286,11 +294,24 @@ kv_attn_kernel(Args args) {
     fresh = ++h == a.H;
     if (fresh) ++share.pair;
   } else {
-    if (!tile_of(a, blockIdx.x, &t)) return;
+    if (!tile_of(a, blockIdx.y, blockIdx.z, &t)) return;
+    t.h = blockIdx.x;
     rec0 = t.rec0;
     rec1 = t.rec1;
     share.unit = share.end;
   }
+
+  // The same in every lane: scalar registers, whatever they were computed in.
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  rec0 = uniform(rec0);
+  rec1 = uniform(rec1);
+  t.rows = uniform(t.rows);
+  t.row0 = uniform(t.row0);
+  t.tok0 = uniform(t.tok0);
+  t.head0 = uniform(t.head0);
+  t.first = uniform(t.first);
+  t.n = uniform(t.n);
+  t.len = uniform(t.len);
 
   // The next record of the wave from `rec` on whose page the table names, as
   // the address of its bytes; null where there is none.
@@ -360,9 +381,9 @@ kv_attn_kernel(Args args) {
   int pos;
   const int64_t base = (int64_t)t.len - t.asked;
   const half8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-  const int row = t.row0 + qcol;
-  const bool in = row < t.rows;
-  const int tok = in ? row / a.share : 0, head = in ? t.h * a.share + row % a.share : 0;
+  const bool in = t.row0 + qcol < t.rows;
+  const int up = by_share(a, t.head0 + qcol), tok = in ? t.tok0 + up : 0;
+  const int head = in ? t.h * a.share + t.head0 + qcol - up * a.share : 0;
   const uint16_t* qp = a.q + (int64_t)(t.first + tok) * a.q_ts + head * a.q_hs;
   pos = in ? (int)max(base + tok, (int64_t)-1) : -1;
 #pragma unroll
@@ -383,9 +404,11 @@ kv_attn_kernel(Args args) {
   // The positions between which every row of the tile sees every token.
   int all0 = 0, all1;
   {
-    const int i0 = t.row0 / a.share, i1 = min(t.row0 + 16 - 1, t.rows - 1) / a.share;
-    all1 = (int)max((int64_t)0, min((int64_t)t.len, base + i0 + 1));
-    if (a.window > 0) all0 = (int)max((int64_t)0, base + i1 + 1 - a.window);
+    const int last = min(t.tok0 + by_share(a, t.head0 + 15), t.n - 1);
+    all1 = (int)max((int64_t)0, min((int64_t)t.len, base + t.tok0 + 1));
+    if (a.window > 0) all0 = (int)max((int64_t)0, base + last + 1 - a.window);
+    all0 = uniform(all0);
+    all1 = uniform(all1);
   }
 
   const float logit = a.scale_log2 * kCodeUnit;
@@ -579,7 +602,7 @@ kv_attn_kernel(Args args) {
     float4v y;
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = fmaf(acc[j][i], kCodeUnit, M[j * 16 / G]) * f;
-    *reinterpret_cast<float4v*>(&so[wave][ocol][16 * j + 4 * oc]) = y;
+    if (t.row0 + ocol < t.rows) *reinterpret_cast<float4v*>(&so[wave][ocol][16 * j + 4 * oc]) = y;
   }
   __syncthreads();
   for (int i = tx; i < 16 * D / 4; i += 64 * kWaves) {
@@ -594,7 +617,7 @@ kv_attn_kernel(Args args) {
       most = fmaxf(most, sm[w][r]);
     }
     if (all_of_it) {
-      store_row(z, t, D, row, d, y, sum, most);
+      store_row(z, t, D, r, d, y, sum, most);
     } else {
       const int p = (slot * z.R + r) * (D + 4) * 4;
       put4(parts_of, p + 4 * d, y);
@@ -607,10 +630,9 @@ kv_attn_kernel(Args args) {
   // order of the parts; where there are many, the last one of each group of
   // them joins the group into its first part, and the last group the groups.
   // Who finds a count full sets it back to 0.
-  const int64_t T = share.T, W = share.W, u0 = head_unit, u1 = u0 + t.units - 1;
-  const int w0 = (int)(((u0 + 1) * W - 1) / T), parts = (int)(((u1 + 1) * W - 1) / T) - w0 + 1;
+  const int w0 = share_with(share, head_unit), parts = share_with(share, head_unit + t.units - 1) - w0 + 1;
   // Workgroup w0 comes to the tile after others unless its share starts there.
-  const int skip = share_start(T, w0, W) != u0;
+  const int skip = share_start(share, w0) != head_unit;
   auto slot_of = [&](int k) { return 2 * (w0 + k) + (k == 0 ? skip : 0); };
   const int g = parts > kOneLevel ? (int)ceilf(sqrtf((float)parts)) : parts, groups = (parts + g - 1) / g;
   int first = ((int)blockIdx.x - w0) / g * g, step = 1, n = min(g, parts - first);
@@ -691,7 +713,7 @@ kv_attn_kernel(Args args) {
         for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], g, y[i]);
       }
       if (last) {
-        store_row(z, t, D, t.row0 + r, d, y, sum, top);
+        store_row(z, t, D, r, d, y, sum, top);
       } else {
         const int p = (slot_of(first) * z.R + r) * (D + 4) * 4;
         put4(parts_of, p + 4 * d, y);
@@ -718,7 +740,7 @@ struct Plan {
 bool plan(const KvDev& c, const AttnCall& a, Plan* p) {
   const int64_t rows = (int64_t)a.max_q * (a.n_heads / c.H), tiles = (rows + 15) / 16, pairs = tiles * a.n_rows;
   p->ids = pairs * c.H;
-  if (p->ids > (1 << 23)) return false;   // a launch has fewer than 2^32 threads
+  if (tiles > 65535 || p->ids > (1 << 23)) return false;   // what a grid holds
   p->tiles = (int)tiles;
   p->R = (int)(rows < 16 ? rows : 16);
   const int64_t room = (int64_t)c.max_pages * c.page_size;
@@ -739,7 +761,8 @@ constexpr size_t kCountBytes = 4 * (2 + 2) * kMaxShares;
 
 template <int D, int G>
 void start(const Args& a, const Plan& p, hipStream_t s) {
-  kv_attn_kernel<D, G><<<(uint32_t)(p.shares ? p.shares : p.ids), 64 * kWaves, 0, s>>>(a);
+  const dim3 grid = p.shares ? dim3(p.shares) : dim3(a.H, a.n_rows, p.tiles);
+  kv_attn_kernel<D, G><<<grid, 64 * kWaves, 0, s>>>(a);
 }
 
 }  // namespace
@@ -774,6 +797,7 @@ hipError_t launch_kv_attention(const KvDev& c, int layer, const AttnCall& call, 
   a.max_q = call.max_q;
   a.H = c.H;
   a.share = call.n_heads / c.H;
+  a.share_magic = (uint32_t)((1ull << 32) / a.share + 1);
   a.window = call.window;
   a.page_shift = c.page_shift;
   a.n_seqs = c.n_seqs;

@@ -16,14 +16,16 @@
 // caches; a load of X then touches a line per row, and from 5 rows on (3 where
 // there are many row tiles) that costs more than staging X in LDS, which the
 // other kernel does.  Kernel times, weights from HBM, groups of 128:
-//   1024 x 4096     B = 1 4.3 us (launch and two trips to memory)
-//   4096 x 4096     B = 1 4.6
-//   4096 x 12288    B = 1 8.8, 3 8.9, 8 11.0, 16 11.2, 32 20.1, 64 39.4
-//   12288 x 4096    B = 1 8.6, 4 9.7, 16 10.2, 32 13.6, 64 25.2
+//   1024 x 4096     B = 1 4.3 us (launch and two trips to memory), 64 12.4
+//   4096 x 4096     B = 1 4.6, 32 9.7, 64 14.4
+//   4096 x 12288    B = 1 8.8, 3 8.9, 8 11.0, 16 11.2, 32 14.7, 64 25.2
+//   12288 x 4096    B = 1 8.6, 4 9.7, 16 10.2, 32 14.3, 64 25.9
 //   131072 x 4096   B = 1 53.8 (groups of 64: 302 MB, 5.6 TB/s), 16 76
-// B = 1 of a large matrix is bound by HBM; the small ones by latency; from B =
-// 16 on by X, which every workgroup reads whole (64 rows of 12288: 1.6 MB for
-// two row tiles; splitting K over workgroups would share it).
+// B = 1 of a large matrix is bound by HBM, of a small one by latency; from B =
+// 16 on by X, which every workgroup reads: a workgroup of four row tiles at B =
+// 64 brings 16 times the bytes of X that it brings of codes, so where there are
+// few row groups each is split along K, and the parts are joined by the last of
+// them to finish.
 
 #include <atomic>
 
@@ -196,33 +198,41 @@ __device__ __forceinline__ void block_product(const u4v (&w)[RT], const uint32_t
   }
 }
 
-// The outputs of S sets of 16 rows (first row 16 T0) from the sums of W waves,
-// added in the waves' order; part[w][set * CT + ct][lane].
-template <int G, int S, int CT, int W>
-__device__ inline void write_outputs(const float4v (*part)[S * CT][64], const uint8_t* codes, const uint32_t* params,
-                                     const uint16_t* X, int64_t ldx, int T0, int N, int K, int B, void* Y,
-                                     int out_f32) {
-  for (int i = threadIdx.x; i < S * CT * 64; i += blockDim.x) {
-    const int l = i & 63, ct = (i >> 6) % CT, rt = (i >> 6) / CT;
-    const int b = 16 * ct + (l & 15);
-    const int64_t n = (int64_t)(T0 + rt) * 16 + 4 * (l >> 4);
-    if (b >= B || n >= N) continue;
-    float4v y = part[0][rt * CT + ct][l];
+// Four outputs of a lane: rows 4 (l / 16) + (0..3) of set `set` (its first row
+// 16 (T0 + set)), row l % 16 of X's tile ct.
+struct Out {
+  const uint8_t* codes;
+  const uint32_t* params;
+  const uint16_t* X;
+  int64_t ldx;
+  void* Y;
+  int N, K, B, G, T0, out_f32;
+};
+__device__ inline void write_four(const Out& o, int set, int ct, int l, float4v y) {
+  const int b = 16 * ct + (l & 15);
+  const int64_t n = (int64_t)(o.T0 + set) * 16 + 4 * (l >> 4);
+  if (b >= o.B) return;
 #pragma unroll
-    for (int k = 1; k < W; ++k) y += part[k][rt * CT + ct][l];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (n + e >= N) break;
-      float v = y[e];
-      if (!(fabsf(v) < __builtin_inff()))
-        v = by_weights(codes, params, K, (K + 127) >> 7, G, X + (int64_t)b * ldx, n + e);
-      const int64_t at = (int64_t)b * N + n + e;
-      if (out_f32)
-        static_cast<float*>(Y)[at] = v;
-      else
-        static_cast<_Float16*>(Y)[at] = (_Float16)v;
-    }
+  for (int e = 0; e < 4; ++e) {
+    if (n + e >= o.N) break;
+    float v = y[e];
+    if (!(fabsf(v) < __builtin_inff()))
+      v = by_weights(o.codes, o.params, o.K, (o.K + 127) >> 7, o.G, o.X + (int64_t)b * o.ldx, n + e);
+    const int64_t at = (int64_t)b * o.N + n + e;
+    if (o.out_f32)
+      static_cast<float*>(o.Y)[at] = v;
+    else
+      static_cast<_Float16*>(o.Y)[at] = (_Float16)v;
   }
+}
+
+// The sum over W waves, in their order, of four outputs.
+template <int W, int S>
+__device__ inline float4v sum_waves(const float4v (*part)[S][64], int i, int l) {
+  float4v y = part[0][i][l];
+#pragma unroll
+  for (int k = 1; k < W; ++k) y += part[k][i][l];
+  return y;
 }
 
 // Few rows of X: every wave reads the inputs of its block from memory in the
@@ -288,32 +298,43 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) part[wave][rt][lane] = acc[rt][0] * kCodeUnit;
   __syncthreads();
-  write_outputs<G, RT, 1, W>(part, codes, params, X, ldx, T0, N, K, B, Y, out_f32);
+  const Out o = {codes, params, X, ldx, Y, N, K, B, G, T0, out_f32};
+  for (int i = threadIdx.x; i < RT * 64; i += 64 * W)
+    write_four(o, i >> 6, 0, i & 63, sum_waves<W, RT>(part, i >> 6, i & 63));
 }
 
 // More rows of X: chunks of 128 WK inputs of all rows go through LDS, whole
 // lines of X from memory and operands from LDS, one chunk computed while the
-// next arrives.  Wave wr WK + wk takes block wk of a chunk and row tile wr of the
-// workgroup's WR.
-template <int G, int CT, int WK, int WR>
+// next arrives.  Wave wr WK + wk takes block wk of a chunk and the row tiles
+// RT wr ..  of the workgroup's RT WR.  Where gridDim.y > 1 a workgroup has a part
+// of the chunks; the last of a row group's workgroups to finish adds the parts
+// in their order and sets the group's count back to 0.
+template <int G, int CT, int WK, int WR, int RT>
 __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __restrict__ codes,
                                                                const uint32_t* __restrict__ params,
                                                                const uint16_t* __restrict__ X, int64_t ldx, int N,
-                                                               int K, int B, void* __restrict__ Y, int out_f32) {
+                                                               int K, int B, void* __restrict__ Y, int out_f32,
+                                                               int32_t* __restrict__ count, float* __restrict__ parts) {
   constexpr int NG = 128 / G, KC = 128 * WK, kThreads = 64 * WK * WR, kRow = KC + 8;   // 16 bytes between rows: all banks
-  constexpr int kLoads = 16 * CT * (KC / 8) / kThreads;
+  constexpr int kLoads = 16 * CT * (KC / 8) / kThreads, S = WR * RT * CT;
   extern __shared__ __align__(16) uint16_t lds[];   // [2][16 CT][kRow], then the waves' sums over it
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wk = wave % WK, wr = wave / WK;
   const int c = lane >> 4, col = lane & 15;
-  const int KB = (K + 127) >> 7, NT = (N + 15) >> 4, chunks = (KB + WK - 1) / WK;
-  const int T0 = blockIdx.x * WR;
-  const int64_t T = min(T0 + wr, NT - 1);
-  const u4v* wp = reinterpret_cast<const u4v*>(codes + T * KB * 1024) + lane;
-  const uint32_t* pp = param_lane<NG>(params, T, KB);
-  float4v acc[1][CT];
+  const int KB = (K + 127) >> 7, NT = (N + 15) >> 4, all = (KB + WK - 1) / WK;
+  const int first = (int)((int64_t)all * blockIdx.y / gridDim.y), chunks = (int)((int64_t)all * (blockIdx.y + 1) / gridDim.y);
+  const int T0 = blockIdx.x * WR * RT;
+  const u4v* wp[RT];
+  const uint32_t* pp[RT];
+  float4v acc[RT][CT];
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) acc[0][ct] = float4v{0, 0, 0, 0};
+  for (int rt = 0; rt < RT; ++rt) {
+    const int64_t T = min(T0 + wr * RT + rt, NT - 1);
+    wp[rt] = reinterpret_cast<const u4v*>(codes + T * KB * 1024) + lane;
+    pp[rt] = param_lane<NG>(params, T, KB);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) acc[rt][ct] = float4v{0, 0, 0, 0};
+  }
 
   // Thread i of the workgroup brings 8 inputs of kLoads rows, of two chunks in
   // turn where the registers allow.
@@ -337,20 +358,24 @@ __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __
       *reinterpret_cast<half8*>(&lds[(buf * 16 * CT + row) * kRow + at % (KC / 8) * 8]) = in[s][i];
     }
   };
-  u4v w[2][1];
-  uint32_t p[2][1];
-  auto load_w = [&](int s, int chunk) {
+  u4v w[2][RT];
+  uint32_t p[2][RT];
+  auto load_w = [&](int s, int rt, int chunk) {
     const int blk = min(chunk * WK + wk, KB - 1);
-    w[s][0] = wp[(int64_t)blk * 64];
-    p[s][0] = pp[(int64_t)blk * NG * 16];
+    w[s][rt] = wp[rt][(int64_t)blk * 64];
+    p[s][rt] = pp[rt][(int64_t)blk * NG * 16];
   };
-  load_w(0, 0);
-  fetch(0, 0);
-  if (kIn == 2 && chunks > 1) fetch(1, 1);
-  load_w(1, 1);
-  stage(0, 0);
+  if (first < chunks) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) load_w(0, rt, first);
+    fetch(0, first);
+    if (kIn == 2 && first + 1 < chunks) fetch(1, first + 1);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) load_w(1, rt, first + 1);
+    stage(0, 0);
+  }
   __syncthreads();
-  for (int chunk0 = 0; chunk0 < chunks; chunk0 += 2) {
+  for (int chunk0 = first; chunk0 < chunks; chunk0 += 2) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int chunk = chunk0 + s;
@@ -364,17 +389,46 @@ __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __
         for (int j = 0; j < 4; ++j)
           x[ct][j] = *reinterpret_cast<const half8*>(&lds[(s * 16 * CT + 16 * ct + col) * kRow + wk * 128 + 32 * j + 8 * c]);
       // Blocks past the last one meet inputs of 0 only.
-      block_product<G, 1, CT>(w[s], p[s], x, acc, [&](int) { load_w(s, chunk + 2); });
+      block_product<G, RT, CT>(w[s], p[s], x, acc, [&](int rt) { load_w(s, rt, chunk + 2); });
       if (more) stage(kIn == 2 ? s ^ 1 : 0, s ^ 1);
       __syncthreads();
     }
   }
-  typedef float4v Part[WR * CT][64];
+  typedef float4v Part[S][64];
   Part* part = reinterpret_cast<Part*>(lds);
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) part[wk][wr * CT + ct][lane] = acc[0][ct] * kCodeUnit;
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) part[wk][(wr * RT + rt) * CT + ct][lane] = acc[rt][ct] * kCodeUnit;
   __syncthreads();
-  write_outputs<G, WR, CT, WK>(part, codes, params, X, ldx, T0, N, K, B, Y, out_f32);
+  const Out o = {codes, params, X, ldx, Y, N, K, B, G, T0, out_f32};
+  if (gridDim.y == 1) {
+    for (int i = threadIdx.x; i < S * 64; i += kThreads)
+      write_four(o, (i >> 6) / CT, (i >> 6) % CT, i & 63, sum_waves<WK, S>(part, i >> 6, i & 63));
+    return;
+  }
+  // [row group][part][S][64]
+  const __amdgpu_buffer_rsrc_t all_parts = __builtin_amdgcn_make_buffer_rsrc(
+      parts + (int64_t)blockIdx.x * gridDim.y * S * 256, 0, gridDim.y * S * 1024, 0x00020000);
+  for (int i = threadIdx.x; i < S * 64; i += kThreads)
+    put4(all_parts, (blockIdx.y * S * 64 + i) * 16, sum_waves<WK, S>(part, i >> 6, i & 63));
+  __shared__ int arrived;
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int before = __hip_atomic_fetch_add(&count[blockIdx.x], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before == (int)gridDim.y - 1)
+      __hip_atomic_store(&count[blockIdx.x], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    arrived = before;
+  }
+  __syncthreads();
+  if (arrived != (int)gridDim.y - 1) return;
+  asm volatile("" ::: "memory");
+  for (int i = threadIdx.x; i < S * 64; i += kThreads) {
+    float4v y = get4(all_parts, i * 16);
+    for (int k = 1; k < (int)gridDim.y; ++k) y += get4(all_parts, (k * S * 64 + i) * 16);
+    write_four(o, (i >> 6) / CT, (i >> 6) % CT, i & 63, y);
+  }
 }
 
 template <int G, int RT, int W, int NB>
@@ -384,29 +438,57 @@ void start_gemv(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, 
       m.codes, reinterpret_cast<const uint32_t*>(m.params), X, ldx, m.n_out, m.n_in, B, Y, out_f32 ? 1 : 0);
 }
 
-template <int G, int CT, int WK, int WR>
-hipError_t start_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
-  const int NT = (m.n_out + 15) / 16;
-  constexpr int kStage = 2 * 16 * CT * (128 * WK + 8) * 2, kPart = WK * WR * CT * 64 * 16;
+// Row groups that K is ever split for, and into how many parts.
+constexpr int kMaxGroups = 256, kMaxParts = 8;
+constexpr size_t kCountBytes = 4 * kMaxGroups;
+
+template <int G, int CT, int WK, int WR, int RT>
+hipError_t start_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, int split, void* ws,
+                      hipStream_t s) {
+  const int NT = (m.n_out + 15) / 16, groups = (NT + WR * RT - 1) / (WR * RT);
+  constexpr int kStage = 2 * 16 * CT * (128 * WK + 8) * 2, kPart = WK * WR * RT * CT * 64 * 16;
   constexpr int kLds = kStage > kPart ? kStage : kPart;
-  static_assert(kLds <= 160 * 1024, "the LDS of a CU");
+  static_assert(kLds <= 160 * 1024 - 64, "the LDS of a CU");
+  const auto kernel = &q4_gemm_kernel<G, CT, WK, WR, RT>;
   static std::atomic<bool> set[64];   // per device: the kernel's limit of LDS is raised
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   if (dev < 0 || dev >= 64 || !set[dev].load(std::memory_order_relaxed)) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_gemm_kernel<G, CT, WK, WR>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (e != hipSuccess) return e;
     if (dev >= 0 && dev < 64) set[dev].store(true, std::memory_order_relaxed);
   }
-  q4_gemm_kernel<G, CT, WK, WR><<<(NT + WR - 1) / WR, 64 * WK * WR, kLds, s>>>(
-      m.codes, reinterpret_cast<const uint32_t*>(m.params), X, ldx, m.n_out, m.n_in, B, Y, out_f32 ? 1 : 0);
+  kernel<<<dim3(groups, split), 64 * WK * WR, kLds, s>>>(
+      m.codes, reinterpret_cast<const uint32_t*>(m.params), X, ldx, m.n_out, m.n_in, B, Y, out_f32 ? 1 : 0,
+      static_cast<int32_t*>(ws), ws ? reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kCountBytes) : nullptr);
   return hipSuccess;
 }
 
+// What a call of B > 16 rows uses: the row tiles of a workgroup, which share its
+// X, and the parts K is split into, so that few row groups fill the chip.
+//   B = 64, us: 4096 x 12288 39.4 in one part, 25.2 in four (44.7 in eight); 65536
+//   x 4096 101 with four row tiles, 71 with eight (one wave two of them; groups
+//   of 32 have no registers for that); 12288 x 4096 25.9 and 31
+struct Shape {
+  int tiles, split;
+};
+Shape shape_of(const Q4Dev& m, int B) {
+  const int NT = (m.n_out + 15) / 16, KB = (m.n_in + 127) / 128;
+  Shape h = {B > 32 && NT >= 2048 && m.group > 32 ? 8 : 4, 1};
+  const int groups = (NT + h.tiles - 1) / h.tiles;
+  if (groups <= kMaxGroups) {
+    h.split = 256 / groups;
+    if (h.split > KB / 8) h.split = KB / 8;
+    if (h.split > kMaxParts) h.split = kMaxParts;
+    if (h.split < 1) h.split = 1;
+  }
+  return h;
+}
+
 template <int G>
-hipError_t start_g(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
+hipError_t start_g(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, void* ws,
+                   hipStream_t s) {
   const int NT = (m.n_out + 15) / 16;
   // Up to 512 row tiles (two a CU) the waves of a workgroup divide K among
   // them; beyond that they also take several row tiles, which share X.
@@ -426,13 +508,14 @@ hipError_t start_g(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* 
     return hipSuccess;
   }
   if (B <= 16)
-    return wide ? start_gemm<G, 1, 4, 4>(m, X, ldx, B, Y, out_f32, s)
-                : start_gemm<G, 1, 16, 1>(m, X, ldx, B, Y, out_f32, s);
-  if (B <= 32)
-    return wide ? start_gemm<G, 2, 4, 4>(m, X, ldx, B, Y, out_f32, s)
-                : start_gemm<G, 2, 8, 1>(m, X, ldx, B, Y, out_f32, s);
-  return wide ? start_gemm<G, 4, 2, 4>(m, X, ldx, B, Y, out_f32, s)
-              : start_gemm<G, 4, 4, 2>(m, X, ldx, B, Y, out_f32, s);
+    return wide ? start_gemm<G, 1, 4, 4, 1>(m, X, ldx, B, Y, out_f32, 1, nullptr, s)
+                : start_gemm<G, 1, 16, 1, 1>(m, X, ldx, B, Y, out_f32, 1, nullptr, s);
+  const Shape h = shape_of(m, B);
+  const int split = ws != nullptr ? h.split : 1;
+  if (B <= 32) return start_gemm<G, 2, 4, 2, 2>(m, X, ldx, B, Y, out_f32, split, ws, s);
+  if constexpr (G > 32)
+    if (h.tiles == 8) return start_gemm<G, 4, 2, 4, 2>(m, X, ldx, B, Y, out_f32, split, ws, s);
+  return start_gemm<G, 4, 2, 4, 1>(m, X, ldx, B, Y, out_f32, split, ws, s);
 }
 
 }  // namespace
@@ -454,11 +537,18 @@ hipError_t launch_q4_unpack(const Q4Dev& m, uint16_t* w, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_q4_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32,
+size_t q4_workspace_bytes(const Q4Dev& m, int B) {
+  if (B <= 16) return 0;
+  const Shape h = shape_of(m, B);
+  const size_t NT = (m.n_out + 15) / 16, groups = (NT + h.tiles - 1) / h.tiles;
+  return h.split > 1 ? kCountBytes + groups * h.split * h.tiles * (B <= 32 ? 2 : 4) * 1024 : 0;
+}
+
+hipError_t launch_q4_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, void* ws,
                           hipStream_t s) {
-  const hipError_t e = m.group == 32   ? start_g<32>(m, X, ldx, B, Y, out_f32, s)
-                       : m.group == 64 ? start_g<64>(m, X, ldx, B, Y, out_f32, s)
-                                       : start_g<128>(m, X, ldx, B, Y, out_f32, s);
+  const hipError_t e = m.group == 32   ? start_g<32>(m, X, ldx, B, Y, out_f32, ws, s)
+                       : m.group == 64 ? start_g<64>(m, X, ldx, B, Y, out_f32, ws, s)
+                                       : start_g<128>(m, X, ldx, B, Y, out_f32, ws, s);
   return e != hipSuccess ? e : hipGetLastError();
 }
 

@@ -116,7 +116,7 @@ tq_status check_attn(const tq_kv_cache* cache, const tq_kv_attn* a, KvDev* d, At
   if (a->n_heads < 1 || a->n_heads % d->H != 0) return TQ_ERR_SHAPE;
   if (a->flags != TQ_OUT_FP16 && a->flags != TQ_OUT_FP32) return TQ_ERR_UNSUPPORTED;
   if (!isfinite(a->scale)) return TQ_ERR_SHAPE;
-  if ((int64_t)a->n_tokens * a->n_heads > INT32_MAX) return TQ_ERR_UNSUPPORTED;
+  if (a->n_heads > TQ_KV_MAX_HEADS || (int64_t)a->n_tokens * a->n_heads > INT32_MAX) return TQ_ERR_UNSUPPORTED;
   c->n_rows = a->n_rows;
   c->n_tokens = a->n_tokens;
   c->max_q = a->max_q < a->n_tokens ? a->max_q : a->n_tokens;
@@ -161,8 +161,14 @@ tq_status tq_q4_unpack_fp16(const tq_q4_matrix* m, uint16_t* w, void* stream) {
   return from_hip(tq::launch_q4_unpack(d, w, (hipStream_t)stream));
 }
 
+size_t tq_q4_workspace_bytes(const tq_q4_matrix* m, int32_t B) {
+  Q4Dev d;
+  if (m == nullptr || B < 1 || B > TQ_Q4_MAX_BATCH || check_q4(m, m->codes, m->params, &d) != TQ_OK) return 0;
+  return tq::q4_workspace_bytes(d, B);
+}
+
 tq_status tq_q4_gemm(const tq_q4_matrix* m, const uint16_t* X, int64_t ldx, int32_t B, void* Y, int32_t flags,
-                     void* stream) {
+                     void* workspace, size_t workspace_bytes, void* stream) {
   if (m == nullptr) return TQ_ERR_NULL;
   Q4Dev d;
   tq_status st = check_q4(m, m->codes, m->params, &d);
@@ -171,7 +177,11 @@ tq_status tq_q4_gemm(const tq_q4_matrix* m, const uint16_t* X, int64_t ldx, int3
   if (X == nullptr || Y == nullptr) return TQ_ERR_NULL;
   if (B < 1 || B > TQ_Q4_MAX_BATCH || ldx < m->n_in) return TQ_ERR_SHAPE;
   if (misaligned(X, 2) || misaligned(Y, 4)) return TQ_ERR_ALIGN;
-  return from_hip(tq::launch_q4_gemm(d, X, ldx, B, Y, flags == TQ_OUT_FP32, (hipStream_t)stream));
+  if (workspace != nullptr) {
+    if (workspace_bytes < tq::q4_workspace_bytes(d, B)) return TQ_ERR_SHAPE;
+    if (misaligned(workspace, 16)) return TQ_ERR_ALIGN;
+  }
+  return from_hip(tq::launch_q4_gemm(d, X, ldx, B, Y, flags == TQ_OUT_FP32, workspace, (hipStream_t)stream));
 }
 
 size_t tq_kv_page_bytes(const tq_kv_cache* cache) {

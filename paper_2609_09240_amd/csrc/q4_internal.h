@@ -20,7 +20,9 @@ struct Q4Dev {
 hipError_t launch_q4_quantize(const uint16_t* w, int64_t ldw, const Q4Dev& m, uint8_t* codes, uint16_t* params,
                               hipStream_t s);
 hipError_t launch_q4_unpack(const Q4Dev& m, uint16_t* w, hipStream_t s);
-hipError_t launch_q4_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s);
+size_t q4_workspace_bytes(const Q4Dev& m, int B);
+hipError_t launch_q4_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, void* ws,
+                          hipStream_t s);
 
 // ---- Cache (kvcache.hip, kvpages.hip, kvattn.hip).
 __host__ __device__ inline int64_t kv_record_bytes(int D, int G) { return 32 * (int64_t)(D + 8 * D / G); }
@@ -107,6 +109,18 @@ __device__ inline half8 code_operand(uint32_t w) {
   const half2v r3 = __builtin_elementwise_fma(__builtin_bit_cast(half2v, t & 0x00F000F0u), b, m);
   return half8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
 }
+// What crosses workgroups is stored and loaded at device scope, past the
+// caches of a die (sc1), so that no cache has to be written back or
+// invalidated: fences around the count of a join cost attention 200 us a call,
+// these 2.
+constexpr int kCoherent = 16;
+__device__ __forceinline__ void put4(__amdgpu_buffer_rsrc_t r, int at, float4v v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, v), r, at, 0, kCoherent);
+}
+__device__ __forceinline__ float4v get4(__amdgpu_buffer_rsrc_t r, int at) {
+  return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, kCoherent));
+}
+
 // Inclusive prefix sum over a wave.
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr 1, 2, 4, 8

@@ -169,7 +169,8 @@ def lib():
             "tq_q4_param_bytes": ([i64, i64, i32], ctypes.c_size_t),
             "tq_q4_quantize": ([vp, i64, qp, vp, vp, vp], ctypes.c_int),
             "tq_q4_unpack_fp16": ([qp, vp, vp], ctypes.c_int),
-            "tq_q4_gemm": ([qp, vp, i64, i32, vp, i32, vp], ctypes.c_int),
+            "tq_q4_workspace_bytes": ([qp, i32], ctypes.c_size_t),
+            "tq_q4_gemm": ([qp, vp, i64, i32, vp, i32, vp, ctypes.c_size_t, vp], ctypes.c_int),
             "tq_kv_page_bytes": ([cp], ctypes.c_size_t),
             "tq_kv_extend": ([cp, vp, vp, i32, vp, vp, vp], ctypes.c_int),
             "tq_kv_free": ([cp, vp, i32, vp, vp], ctypes.c_int),
@@ -567,13 +568,34 @@ def quantize_linear(W, f2=0.1, iters=4, host_rowptr=True, group_offsets=False, s
 # Products with 4-bit weights.
 # --------------------------------------------------------------------------
 
+class _Workspaces:
+    """Workspaces whose counts are zeros between calls: one per stream, kept
+    with the handle that owns it and made anew, larger, when a call needs more.
+    Under graph capture every call gets one of its own, filled in the graph."""
+
+    __slots__ = ("device", "by_stream")
+
+    def __init__(self, device):
+        self.device, self.by_stream = device, {}
+
+    def get(self, need, stream):
+        key = _stream(stream)
+        ws = self.by_stream.get(key)
+        if ws is None or ws.numel() < need:
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
+                if not torch.cuda.is_current_stream_capturing():
+                    self.by_stream[key] = ws
+        return ws
+
+
 class Q4Linear:
     """A matrix of 4-bit weights in device memory (the buffers tq_q4_matrix
     points at): codes uint8, params float16, both flat and in the library's
     layout.  The buffers are fixed when it is made; their contents may
     change."""
 
-    __slots__ = ("n_out", "n_in", "group", "codes", "params", "_ref")
+    __slots__ = ("n_out", "n_in", "group", "codes", "params", "_ref", "_ws")
 
     def __init__(self, n_out, n_in, group, codes, params):
         _cuda(codes, torch.uint8, "codes")
@@ -585,6 +607,7 @@ class Q4Linear:
             raise ValueError(f"codes and params must hold {nc} and {np_} bytes")
         self.n_out, self.n_in, self.group, self.codes, self.params = n_out, n_in, group, codes, params
         self._ref = ctypes.pointer(TqQ4Matrix(n_out, n_in, group, 0, codes.data_ptr(), params.data_ptr()))
+        self._ws = _Workspaces(codes.device)
 
     @classmethod
     def empty(cls, n_out, n_in, group=GROUP, device="cuda"):
@@ -633,9 +656,14 @@ def _out_buffer(t, shape, dtype, name):
     _cuda(t, dtype, name)
 
 
-def tq_q4_gemm(mat, X, Y=None, out_f32=False, stream=None):
+def tq_q4_workspace_bytes(mat, B):
+    """Workspace with which tq_q4_gemm of B rows is fastest."""
+    return int(lib().tq_q4_workspace_bytes(mat._ref, B))
+
+
+def tq_q4_gemm(mat, X, Y=None, out_f32=False, workspace=None, stream=None):
     """Y = X W^T for fp16 X [B, K] (or x [K]), B up to Q4_MAX_BATCH; Y [B, N]
-    (or [N])."""
+    (or [N]).  A workspace of the caller's is zeros before its first call."""
     one = X.dim() == 1
     if one:
         X = X.unsqueeze(0)
@@ -649,9 +677,16 @@ def tq_q4_gemm(mat, X, Y=None, out_f32=False, stream=None):
         Y = torch.empty(shape, dtype=dtype, device=X.device)
     else:
         _out_buffer(Y, shape, dtype, "Y")
+    if workspace is not None:
+        _cuda(workspace, torch.uint8, "workspace")
+    elif B > 16:
+        need = lib().tq_q4_workspace_bytes(mat._ref, B)
+        workspace = mat._ws.get(need, stream) if need else None
     _check(lib().tq_q4_gemm(mat._ref, X.data_ptr(), ldx, B, Y.data_ptr(), OUT_FP32 if out_f32 else OUT_FP16,
-                            _stream(stream)), "tq_q4_gemm")
-    _used_on(stream, X, Y, mat.codes, mat.params)
+                            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
+           "tq_q4_gemm")
+    if stream is not None:
+        _used_on(stream, X, Y, workspace, mat.codes, mat.params)
     return Y
 
 
@@ -667,7 +702,7 @@ class KVCache:
     calls below.  One cache serves one stream at a time: calls on another
     one are the caller's to order."""
 
-    __slots__ = ("data", "pages", "lens", "refs", "n_kv_heads", "head_dim", "page_size", "group", "_ref", "_attn_ws")
+    __slots__ = ("data", "pages", "lens", "refs", "n_kv_heads", "head_dim", "page_size", "group", "_ref", "_ws")
 
     def __init__(self, data, pages, lens, refs, n_kv_heads, head_dim, page_size=64, group=64):
         _cuda(data, torch.uint8, "data")
@@ -687,7 +722,7 @@ class KVCache:
         self.data, self.pages, self.lens, self.refs = data, pages, lens, refs
         self.n_kv_heads, self.head_dim, self.page_size, self.group = n_kv_heads, head_dim, page_size, group
         self._ref = ref
-        self._attn_ws = {}   # stream -> workspace of tq_kv_attention, zeros when made
+        self._ws = _Workspaces(data.device)
 
     @classmethod
     def empty(cls, n_layers, n_pages, n_seqs, max_pages, n_kv_heads, head_dim, page_size=64, group=64,
@@ -703,15 +738,9 @@ class KVCache:
                    n_kv_heads, head_dim, page_size, group)
 
     def attention_workspace(self, need, stream=None):
-        """A workspace of at least `need` bytes for tq_kv_attention on a stream
-        (the current one without): one per stream, kept with the cache and
-        made anew, larger, when a call needs more."""
-        key = _stream(stream)
-        ws = self._attn_ws.get(key)
-        if ws is None or ws.numel() < need:
-            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-                ws = self._attn_ws[key] = torch.zeros(need, dtype=torch.uint8, device=self.data.device)
-        return ws
+        """The workspace of at least `need` bytes that tq_kv_attention uses on a
+        stream (the current one without) unless it is given one."""
+        return self._ws.get(need, stream)
 
     def _buffers(self):
         return self.data, self.pages, self.lens, self.refs

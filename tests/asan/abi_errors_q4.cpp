@@ -90,7 +90,7 @@ int main() {
     expect("param bytes of group 16", (int)tq_q4_param_bytes(33, 300, 16), 0);
     const uint16_t* X = fake<const uint16_t>();
     auto gemm = [&](const tq_q4_matrix& m, const uint16_t* x, int64_t ldx, int B, void* y, int flags) {
-      return (int)tq_q4_gemm(&m, x, ldx, B, y, flags, nullptr);
+      return (int)tq_q4_gemm(&m, x, ldx, B, y, flags, nullptr, 0, nullptr);
     };
     void* Y = fake<void>();
     tq_q4_matrix m = mat();
@@ -111,7 +111,7 @@ int main() {
     expect("q4 flags", gemm(m, X, 300, 1, Y, 2), TQ_ERR_UNSUPPORTED);
     expect("q4 X align", gemm(m, reinterpret_cast<const uint16_t*>(kFake + 1), 300, 1, Y, 0), TQ_ERR_ALIGN);
     expect("q4 Y align", gemm(m, X, 300, 1, fake<void>(2), 0), TQ_ERR_ALIGN);
-    expect("q4 matrix", tq_q4_gemm(nullptr, X, 300, 1, Y, 0, nullptr), TQ_ERR_NULL);
+    expect("q4 matrix", tq_q4_gemm(nullptr, X, 300, 1, Y, 0, nullptr, 0, nullptr), TQ_ERR_NULL);
     expect("q4 quantize w", tq_q4_quantize(nullptr, 300, &m, fake<uint8_t>(), fake<uint16_t>(), nullptr), TQ_ERR_NULL);
     expect("q4 quantize ldw", tq_q4_quantize(X, 299, &m, fake<uint8_t>(), fake<uint16_t>(), nullptr), TQ_ERR_SHAPE);
     expect("q4 quantize codes", tq_q4_quantize(X, 300, &m, nullptr, fake<uint16_t>(), nullptr), TQ_ERR_NULL);

@@ -149,6 +149,48 @@ def test_outputs_that_are_not_finite():
     np.testing.assert_array_equal(got[inf], want[inf])
 
 
+@pytest.mark.parametrize("n,k,B,group", [(100, 4096, 17, 64), (1000, 5000, 40, 32), (4096, 2048, 64, 128),
+                                         (33000, 1024, 64, 64), (16, 16384, 32, 128)])
+def test_split_along_k(n, k, B, group):
+    """Parts of K joined in one launch: exact sums are equal with and without
+    a workspace, and a workspace serves call after call and other shapes."""
+    r = np.random.default_rng(n)
+    ng = -(-k // group)
+    codes = r.integers(0, 16, (n, k)).astype(np.uint8)
+    s = r.choice([0.25, 0.5, -0.5], (n, ng)).astype(np.float16)
+    m = r.integers(-8, 9, (n, ng)).astype(np.float16)
+    x = r.integers(-1, 2, (B, k)).astype(np.float16)
+    mat, xd = _upload(codes, s, m, group), torch.from_numpy(x).cuda()
+    want = q4.gemm(codes, s, m, group, x)
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    for b in (B, 17, B):
+        for kw in (dict(workspace=ws), dict()):
+            y = tq.tq_q4_gemm(mat, xd[:b], out_f32=True, **kw)
+            np.testing.assert_array_equal(y.cpu().numpy().astype(np.float64), want[:b])
+    y = torch.empty((B, n), dtype=torch.float32, device="cuda")
+    tq._check(tq.lib().tq_q4_gemm(mat._ref, xd.data_ptr(), k, B, y.data_ptr(), 1, None, 0, tq._stream(None)), "gemm")
+    np.testing.assert_array_equal(y.cpu().numpy().astype(np.float64), want)
+
+
+def test_split_along_k_from_a_graph():
+    codes, s, m = _random(300, 4096, 64, 2)
+    mat = _upload(codes, s, m, 64)
+    x = torch.randn((40, 4096), dtype=torch.float16, device="cuda")
+    y = torch.empty((40, 300), dtype=torch.float16, device="cuda")
+    tq.tq_q4_gemm(mat, x, Y=y)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        tq.tq_q4_gemm(mat, x, Y=y)
+    for i in range(4):
+        x.copy_(torch.randn((40, 4096), device="cuda"))
+        want = tq.tq_q4_gemm(mat, x)
+        y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), i
+
+
 def test_on_another_stream():
     codes, s, m = _random(64, 512, 128, 1)
     mat = _upload(codes, s, m, 128)
@@ -189,6 +231,13 @@ def test_refusals():
     with pytest.raises(tq.TqError) as e:
         tq.tq_q4_gemm(mat, x)
     assert e.value.status == 2
+    assert tq.tq_q4_workspace_bytes(mat, 16) == 0 and tq.tq_q4_workspace_bytes(mat, 65) == 0
+    deep = tq.Q4Linear.empty(32, 4096, 64)
+    wide = torch.zeros((64, 4096), dtype=torch.float16, device="cuda")
+    for ws in (torch.zeros(tq.tq_q4_workspace_bytes(deep, 64) - 16, dtype=torch.uint8, device="cuda"),):
+        with pytest.raises(tq.TqError) as e:
+            tq.tq_q4_gemm(deep, wide, workspace=ws)
+        assert e.value.status == 2
     for bad in (x[:2].float(), x[:2, :100], x[:2].t(), x[:2].cpu()):
         with pytest.raises(ValueError):
             tq.tq_q4_gemm(mat, bad)
