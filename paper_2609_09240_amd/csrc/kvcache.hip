@@ -79,14 +79,16 @@ __global__ void __launch_bounds__(kOne ? 64 : 256) kv_append_kernel(KvDev c, int
     if (lead && d_err) atomicAdd(d_err, 1);
     return;
   }
-  if (lead && d_err) {
+  if (blockIdx.x == 0 && h == 0 && d_err) {
     // A row counts once: what it may not write, or has no page for.
-    bool bad = r.over;
-    for (int64_t s = r.start >> c.page_shift; !bad && r.n > 0 && s <= ((int64_t)r.start + r.n - 1) >> c.page_shift; ++s) {
+    int bad = r.over;
+    const int64_t s0 = r.start >> c.page_shift, s1 = r.n > 0 ? ((int64_t)r.start + r.n - 1) >> c.page_shift : s0 - 1;
+    for (int64_t s = s0 + threadIdx.x; s <= s1; s += blockDim.x) {
       const int page = s < c.max_pages ? c.pages[(int64_t)r.seq * c.max_pages + s] : -1;
-      bad = page < 0 || page >= c.n_pages;
+      bad |= page < 0 || page >= c.n_pages;
     }
-    if (bad) atomicAdd(d_err, 1);
+    bad = __syncthreads_or(bad);
+    if (lead && bad) atomicAdd(d_err, 1);
   }
   const int64_t rec = (r.start >> 5) + blockIdx.x;
   const int t0 = (int)max((int64_t)0, r.start - rec * 32);                             // new tokens of the record: [t0, t1)

@@ -134,11 +134,14 @@ __device__ __attribute__((noinline)) float by_weights(const uint8_t* codes, cons
   const int64_t T = n >> 4;
   const int r = (int)(n & 15);
   float acc = 0.0f;
-  for (int k = 0; k < K; ++k) {
-    const int blk = k >> 7, j = (k >> 5) & 3, c = (k >> 3) & 3, e = k & 7;
+  for (int k = 0; k < K && acc == acc; k += 8) {   // NaN stays
+    const int blk = k >> 7, j = (k >> 5) & 3, c = (k >> 3) & 3;
     const uint32_t w = cw[((T * KB + blk) * 64 + c * 16 + r) * 4 + j];
     const uint32_t p = pw[(T * KB * (128 / G) + k / G) * 16 + r];
-    acc = fmaf(q4_value((w >> (4 * nibble_of(e))) & 15u, lo_half(p), hi_half(p)), lo_half(x[k]), acc);
+    const half8 v = load_tail(x, k, K);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (k + e < K) acc = fmaf(q4_value((w >> (4 * nibble_of(e))) & 15u, lo_half(p), hi_half(p)), (float)v[e], acc);
   }
   return acc;
 }

@@ -112,6 +112,16 @@ int main() {
     expect("q4 X align", gemm(m, reinterpret_cast<const uint16_t*>(kFake + 1), 300, 1, Y, 0), TQ_ERR_ALIGN);
     expect("q4 Y align", gemm(m, X, 300, 1, fake<void>(2), 0), TQ_ERR_ALIGN);
     expect("q4 matrix", tq_q4_gemm(nullptr, X, 300, 1, Y, 0, nullptr, 0, nullptr), TQ_ERR_NULL);
+    {
+      tq_q4_matrix deep = mat();
+      deep.n_in = 4096;
+      const size_t need = tq_q4_workspace_bytes(&deep, 64);
+      expect("q4 workspace", need > 0, 1);
+      expect("q4 workspace of few rows", (int)tq_q4_workspace_bytes(&deep, 16), 0);
+      expect("q4 workspace of 65 rows", (int)tq_q4_workspace_bytes(&deep, 65), 0);
+      expect("q4 workspace size", tq_q4_gemm(&deep, X, 4096, 64, Y, 0, fake<void>(), need - 1, nullptr), TQ_ERR_SHAPE);
+      expect("q4 workspace align", tq_q4_gemm(&deep, X, 4096, 64, Y, 0, fake<void>(8), need, nullptr), TQ_ERR_ALIGN);
+    }
     expect("q4 quantize w", tq_q4_quantize(nullptr, 300, &m, fake<uint8_t>(), fake<uint16_t>(), nullptr), TQ_ERR_NULL);
     expect("q4 quantize ldw", tq_q4_quantize(X, 299, &m, fake<uint8_t>(), fake<uint16_t>(), nullptr), TQ_ERR_SHAPE);
     expect("q4 quantize codes", tq_q4_quantize(X, 300, &m, nullptr, fake<uint16_t>(), nullptr), TQ_ERR_NULL);
@@ -193,6 +203,7 @@ int main() {
     a = attn(); a.max_q = 0; expect("max_q", attend(c, a), TQ_ERR_SHAPE);
     a = attn(); a.max_len = -1; expect("max_len", attend(c, a), TQ_ERR_SHAPE);
     a = attn(); a.window = -1; expect("window", attend(c, a), TQ_ERR_SHAPE);
+    a = attn(); a.n_heads = 4 * 16384; expect("query heads", attend(c, a), TQ_ERR_UNSUPPORTED);
     a = attn(); a.flags = 3; expect("attention flags", attend(c, a), TQ_ERR_UNSUPPORTED);
     a = attn(); a.scale = NAN; expect("scale", attend(c, a), TQ_ERR_SHAPE);
     a = attn(); a.n_tokens = 1 << 28; expect("o past 2^31 rows", attend(c, a), TQ_ERR_UNSUPPORTED);

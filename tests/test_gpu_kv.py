@@ -131,6 +131,26 @@ def test_append_refuses_and_counts():
     np.testing.assert_allclose(a.cpu().numpy(), q4.values(c, s, m, 64), rtol=2.0 ** -11, atol=2.0 ** -24)
 
 
+def test_append_counts_a_row_once_over_many_pages():
+    """Pages missing here and there among the 40 that a row writes: the row
+    counts once, what has pages is written."""
+    cache = tq.KVCache.empty(1, 50, 1, 45, 1, 64, 32, 32)
+    starts = tq.tq_kv_extend(cache, cu_new=_i(0, 1280))
+    k = torch.from_numpy(rows((1280, 1, 64), 1)).cuda()
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    tq.tq_kv_append(cache, 0, k, k, starts, cu_new=_i(0, 1280), max_new=1280, d_err=err)
+    assert int(err) == 0
+    want, _ = tq.tq_kv_read(cache, 0, starts, 1280, cu_new=_i(0, 1280), max_new=1280)
+    cache.data.fill_(0)
+    cache.pages[0, [3, 39]] = -1
+    tq.tq_kv_append(cache, 0, k, k, starts, cu_new=_i(0, 1280), max_new=1280, d_err=err)
+    assert int(err) == 1
+    got, _ = tq.tq_kv_read(cache, 0, starts, 1280, cu_new=_i(0, 1280), max_new=1280)
+    want[96:128] = 0
+    want[39 * 32:] = 0
+    assert torch.equal(got, want)
+
+
 class Both:
     """A cache on the GPU and its table in the oracle."""
 
