@@ -28,12 +28,12 @@
 // SIMD.  One token over one long cache: 5.4 TB/s for every further byte, and
 // 6 us of launch, table, first loads and joining waves before the first, 7 us
 // for joining 96 parts a head.
-//   1 x 131072 tokens, 8 heads, groups of 128 (143 MB)  39.3 us
-//   32 ragged rows to 8192, groups of 64 (93 MB)        32.2
+//   1 x 131072 tokens, 8 heads, groups of 128 (143 MB)  40.3 us
+//   32 ragged rows to 8192, groups of 64 (93 MB)        33.2
 //   1 x 4096 (4.7 MB)                                   11.8
-//   1 x 45                                              6.5
+//   1 x 45                                              6.4
 //   a chunk of 2 x 1000 queries over up to 5000, window 2048, 14 heads of 64 on
-//   2, groups of 32 (10 GFLOP)                          68
+//   2, groups of 32 (10 GFLOP)                          77
 // (One launch a split and another to join: 31 + 6.5, 33 + 6 and 10 + 6 for the
 // first three, and 3 us between the launches.  32 or 64 rows a tile, which
 // unpack a record once for two or four tiles, halve the waves: 90 and 120 us

@@ -6,9 +6,10 @@
 // of theirs holds 8 tokens of one channel.  A word that also holds tokens
 // that are not new is read, changed and written back by one thread.
 //
-// 6000 tokens of 8 heads of 128 in groups of 32 (49 MB in, 15 MB out): 13.3 us,
-// 4.8 TB/s, bound by the arithmetic of the codes (20.4 us with a division a
-// value); read back 11.5 us, 5.6 TB/s.  One token each of 64 rows: 5.3 and 3.7
+// 6000 tokens of 8 heads of 128 in groups of 32 (24.6 MB in, 7.7 MB out): 15.0
+// us, 2.1 TB/s (13.5 at best), bound by the arithmetic of the codes, which takes
+// 59 % of the vector slots (a division a value took 1.5 times as long); read
+// back 13.4 us, 2.4 TB/s, 47 % of them.  One token each of 64 rows: 5.6 and 4.1
 // us, the launch and three trips to memory one after the other.
 
 #include "q4_internal.h"

@@ -9,10 +9,11 @@
 // in which atomics reach them does not show.
 //
 // The deciding launches are bound by their trips to memory, one after the other
-// (slots, lengths, last pages, counts of pages): 60 forks 7.6 us, room for 32
-// rows 5.2 us, a compaction's plan 2.6 us, freeing 2 to 3 us.  The copies are
-// bound by HBM: 53 MB to and fro in 9.6 us, half of it from the caches, 64 MB of
-// a compaction in 19.7 us, 6.5 TB/s.  (1024 threads for any number of rows: 9.6
+// (slots, lengths, last pages, counts of pages): 60 forks 7.9 us, room for 32
+// rows 5.7 us, a compaction's plan 2.8 us, freeing 2 to 4 us.  The copies are
+// bound by HBM: 53 MB written in 11.2 us (4.8 TB/s; what is read is 7 MB of
+// shared pages and the caches), 64 MB of a compaction read and written in 23.7,
+// 5.4 TB/s.  (1024 threads for any number of rows: 9.6
 // and 7.0 us; the free pages of a thread handed out one after the other: 11.6.)
 
 #include "q4_internal.h"

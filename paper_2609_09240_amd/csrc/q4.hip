@@ -16,11 +16,11 @@
 // caches; a load of X then touches a line per row, and from 5 rows on (3 where
 // there are many row tiles) that costs more than staging X in LDS, which the
 // other kernel does.  Kernel times, weights from HBM, groups of 128:
-//   1024 x 4096     B = 1 4.3 us (launch and two trips to memory), 64 12.4
+//   1024 x 4096     B = 1 4.0 us (launch and two trips to memory), 64 12.4
 //   4096 x 4096     B = 1 4.6, 32 9.7, 64 14.4
-//   4096 x 12288    B = 1 8.8, 3 8.9, 8 11.0, 16 11.2, 32 14.7, 64 25.2
+//   4096 x 12288    B = 1 8.8, 3 8.9, 8 11.0, 16 11.6, 32 14.7, 64 25.2
 //   12288 x 4096    B = 1 8.6, 4 9.7, 16 10.2, 32 14.3, 64 25.9
-//   131072 x 4096   B = 1 53.8 (groups of 64: 302 MB, 5.6 TB/s), 16 76
+//   131072 x 4096   B = 1 52.7 (groups of 64: 302 MB, 5.7 TB/s), 16 76
 // B = 1 of a large matrix is bound by HBM, of a small one by latency; from B =
 // 16 on by X, which every workgroup reads: a workgroup of four row tiles at B =
 // 64 brings 16 times the bytes of X that it brings of codes, so where there are
