@@ -378,6 +378,11 @@ tq_status tq_gemv_chain(const void* plan, void* sync, const tq_chain_info* info,
 #define TQ_KV_MAX_ROWS 1024     /* rows of a call that changes the page table */
 #define TQ_KV_MAX_PAGES (1 << 20)   /* pages of one sequence */
 #define TQ_KV_MAX_HEADS 65520       /* query heads in tq_kv_attention */
+/* The workspaces of tq_q4_gemm and tq_kv_attention hold counts that every
+ * call finds and leaves 0, all of them in the first TQ_WORKSPACE_COUNT_BYTES
+ * (or in all of a smaller one): only those are to be filled with zeros, once,
+ * before a workspace's first call. */
+#define TQ_WORKSPACE_COUNT_BYTES 16384
 
 /* Non-owning view of a matrix of 4-bit weights.  N and K may be any sizes;
  * the last tile of rows and the last 128 inputs are filled up with codes and
@@ -419,9 +424,9 @@ size_t tq_q4_workspace_bytes(const tq_q4_matrix* m, int32_t B);
  *   Y  [B][N], fp16 (TQ_OUT_FP16) or fp32 (TQ_OUT_FP32); 4-byte aligned
  *   workspace  NULL, or tq_q4_workspace_bytes of the same arguments (0 for
  *      most), 16-byte aligned: with it K is split among workgroups where more
- *      than 16 rows meet few outputs.  It holds counts that every call finds
- *      and leaves 0: it is filled with zeros once, before its first call, and
- *      serves any calls that do not overlap in time.
+ *      than 16 rows meet few outputs.  Its counts (TQ_WORKSPACE_COUNT_BYTES)
+ *      are filled with zeros once; it serves any calls that do not overlap in
+ *      time.
  * scale * sum(code * x) + offset * sum(x) per group, every product exact,
  * sums in fp32; a row's result depends on the row, on the range of B (1 or 2,
  * 3 or 4, 5..16, 17..32, 33..64) and on whether there is a workspace, not on
@@ -568,9 +573,8 @@ tq_status tq_kv_read(const tq_kv_cache* cache, int32_t layer, const int32_t* seq
  * enters the matrix instructions as two fp16 numbers, 22 bits of it.
  * The workspace (16-byte aligned, tq_kv_attention_workspace_bytes of the same
  * arguments, which may be 0) holds what the parts of a long cache give, and
- * counts of them that every call finds and leaves 0: it is filled with zeros
- * once, before its first call, and serves any calls that do not overlap in
- * time. */
+ * counts of them (TQ_WORKSPACE_COUNT_BYTES, filled with zeros once); it serves
+ * any calls that do not overlap in time. */
 typedef struct tq_kv_attn {
   int32_t n_rows;           /* >= 1 */
   int32_t n_tokens;         /* tokens of q and o, >= 1 */

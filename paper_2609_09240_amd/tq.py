@@ -26,6 +26,7 @@ MAX_GROUPED = 8
 MAX_BATCH = 64
 Q4_MAX_BATCH = 64
 KV_MAX_ROWS = 1024
+WORKSPACE_COUNT_BYTES = 16384   # at the front of a 4-bit operator's workspace
 
 STATUS = {0: "TQ_OK", 1: "TQ_ERR_NULL", 2: "TQ_ERR_SHAPE", 3: "TQ_ERR_ALIGN",
           4: "TQ_ERR_UNSUPPORTED", 5: "TQ_ERR_HIP"}
@@ -571,21 +572,28 @@ def quantize_linear(W, f2=0.1, iters=4, host_rowptr=True, group_offsets=False, s
 class _Workspaces:
     """Workspaces whose counts are zeros between calls: one per stream, kept
     with the handle that owns it and made anew, larger, when a call needs more.
-    Under graph capture every call gets one of its own, filled in the graph."""
+    Under graph capture every call gets one of its own from the graph's memory,
+    its counts filled in the graph: a replay may come when the stream's buffer
+    has been replaced, or run beside a call that uses it."""
 
     __slots__ = ("device", "by_stream")
 
     def __init__(self, device):
         self.device, self.by_stream = device, {}
 
+    def _new(self, need):
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        ws[:WORKSPACE_COUNT_BYTES].zero_()
+        return ws
+
     def get(self, need, stream):
-        key = _stream(stream)
-        ws = self.by_stream.get(key)
-        if ws is None or ws.numel() < need:
-            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-                ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
-                if not torch.cuda.is_current_stream_capturing():
-                    self.by_stream[key] = ws
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            if torch.cuda.is_current_stream_capturing():
+                return self._new(need)
+            key = _stream(stream)
+            ws = self.by_stream.get(key)
+            if ws is None or ws.numel() < need:
+                ws = self.by_stream[key] = self._new(need)
         return ws
 
 
@@ -663,7 +671,8 @@ def tq_q4_workspace_bytes(mat, B):
 
 def tq_q4_gemm(mat, X, Y=None, out_f32=False, workspace=None, stream=None):
     """Y = X W^T for fp16 X [B, K] (or x [K]), B up to Q4_MAX_BATCH; Y [B, N]
-    (or [N]).  A workspace of the caller's is zeros before its first call."""
+    (or [N]).  A workspace of the caller's has zeros in its first
+    WORKSPACE_COUNT_BYTES before its first call."""
     one = X.dim() == 1
     if one:
         X = X.unsqueeze(0)
@@ -739,7 +748,8 @@ class KVCache:
 
     def attention_workspace(self, need, stream=None):
         """The workspace of at least `need` bytes that tq_kv_attention uses on a
-        stream (the current one without) unless it is given one."""
+        stream (the current one without) unless it is given one; while that
+        stream is being captured, a new one for the graph."""
         return self._ws.get(need, stream)
 
     def _buffers(self):
@@ -869,7 +879,8 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=1, max_len=0, s
     """Attention of q [T, n_heads, D], the last tokens of their slots, over the
     cache: o [T, n_heads, D] (fp16 or fp32), and with want_lse also the log of
     the softmax's sum, fp32 [T, n_heads].  scale: 1 / sqrt(D) without.  A
-    workspace of the caller's is zeros before its first call."""
+    workspace of the caller's has zeros in its first WORKSPACE_COUNT_BYTES
+    before its first call."""
     T, n_heads, D = q.shape
     n = seqs.numel() if seqs is not None else (cu_q.numel() - 1 if cu_q is not None else T)
     if cu_q is None and n != T:
