@@ -379,9 +379,9 @@ tq_status tq_gemv_chain(const void* plan, void* sync, const tq_chain_info* info,
 #define TQ_KV_MAX_PAGES (1 << 20)   /* pages of one sequence */
 #define TQ_KV_MAX_HEADS 65520       /* query heads in tq_kv_attention */
 /* The workspaces of tq_q4_gemm and tq_kv_attention hold counts that every
- * call finds and leaves 0, all of them in the first TQ_WORKSPACE_COUNT_BYTES
- * (or in all of a smaller one): only those are to be filled with zeros, once,
- * before a workspace's first call. */
+ * call finds and leaves 0, all of them in the first TQ_WORKSPACE_COUNT_BYTES:
+ * only those are to be filled with zeros, once, before a workspace's first
+ * call.  One that is large enough serves calls of both. */
 #define TQ_WORKSPACE_COUNT_BYTES 16384
 
 /* Non-owning view of a matrix of 4-bit weights.  N and K may be any sizes;

@@ -757,8 +757,8 @@ bool plan(const KvDev& c, const AttnCall& a, Plan* p) {
 }
 
 // Two counts for each of the two parts that a share can leave.
-constexpr size_t kCountBytes = 4 * (2 + 2) * kMaxShares;
-static_assert(kCountBytes <= TQ_WORKSPACE_COUNT_BYTES, "all counts at the front");
+constexpr size_t kCountBytes = TQ_WORKSPACE_COUNT_BYTES;
+static_assert(4 * (2 + 2) * kMaxShares <= kCountBytes, "all counts at the front");
 
 template <int D, int G>
 void start(const Args& a, const Plan& p, hipStream_t s) {

@@ -443,8 +443,10 @@ void start_gemv(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, 
 
 // Row groups that K is ever split for, and into how many parts.
 constexpr int kMaxGroups = 256, kMaxParts = 8;
-constexpr size_t kCountBytes = 4 * kMaxGroups;
-static_assert(kCountBytes <= TQ_WORKSPACE_COUNT_BYTES, "all counts at the front");
+// The parts begin behind every count that any operator keeps, so that one
+// workspace serves products and attention.
+constexpr size_t kCountBytes = TQ_WORKSPACE_COUNT_BYTES;
+static_assert(4 * kMaxGroups <= kCountBytes, "all counts at the front");
 
 template <int G, int CT, int WK, int WR, int RT>
 hipError_t start_gemm(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, int split, void* ws,

@@ -84,3 +84,21 @@ def test_only_the_counts_need_zeros():
     for _ in range(3):
         y = tq.tq_q4_gemm(mat, torch.from_numpy(x).cuda(), out_f32=True, workspace=ws)
         np.testing.assert_array_equal(y.cpu().numpy().astype(np.float64), q4.gemm(codes, s, mn, 64, x))
+
+
+def test_one_workspace_for_products_and_attention():
+    """The parts that one leaves are not the counts of the other."""
+    m = Model([5000, 4000, 77], 2, 128, 64, 64)
+    q = torch.from_numpy(rows((3, 32, 128), 1)).cuda()
+    mat = tq.tq_q4_quantize(torch.randn((300, 8192), device="cuda").half(), 64)
+    x = torch.randn((64, 8192), device="cuda").half()
+    o, y = tq.tq_kv_attention(m.cache, 0, q), tq.tq_q4_gemm(mat, x)
+    assert tq.tq_q4_workspace_bytes(mat, 64) > tq.WORKSPACE_COUNT_BYTES
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        got_y = torch.full_like(y, 9.0)
+        tq.tq_q4_gemm(mat, x, Y=got_y, workspace=ws)
+        got_o = torch.full_like(o, 9.0)
+        tq.tq_kv_attention(m.cache, 0, q, o=got_o, workspace=ws)
+        assert torch.equal(got_y, y) and torch.equal(got_o, o)
+        assert bool((ws[:tq.WORKSPACE_COUNT_BYTES] == 0).all())
