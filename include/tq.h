@@ -570,7 +570,9 @@ tq_status tq_kv_read(const tq_kv_cache* cache, int32_t layer, const int32_t* seq
  *   o        [n_tokens][n_heads][D], fp16 or fp32 per flags; 16-byte aligned
  *   lse      fp32 [n_tokens][n_heads], may be NULL
  * Products are exact, the softmax, its sums and o's are fp32; a probability
- * enters the matrix instructions as two fp16 numbers, 22 bits of it.
+ * times the scale of a value enters the matrix instructions as two fp16
+ * numbers, 22 bits of it; what lies below 2^-37 of the largest probability
+ * times the group's largest scale is rounded off.
  * The workspace (16-byte aligned, tq_kv_attention_workspace_bytes of the same
  * arguments, which may be 0) holds what the parts of a long cache give, and
  * counts of them (TQ_WORKSPACE_COUNT_BYTES, filled with zeros once); it serves

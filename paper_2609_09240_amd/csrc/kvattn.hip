@@ -14,7 +14,8 @@
 //   its operand of the second product as they stand, since values are stored
 //   with those eight tokens in one word: O^T += V^T P^T.
 // A probability times a value scale enters as two fp16 numbers (hi + lo, 22
-// bits); the sums of p, of p mv and of everything else are fp32.
+// bits), in a unit of the row and group that follows the largest scale seen;
+// the sums of p, of p mv and of everything else are fp32.
 //
 // Work split: a workgroup has four waves that take the records of its range
 // in turn and join their references, sums and outputs through LDS.  Where there
@@ -64,15 +65,43 @@ __device__ inline float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// What a probability is scaled by: the running reference r of a row (log2) is
-// kept so that exp2(s - r) of its largest logit so far lies in 2^8 .. 2^10.
-// Their products with the value scales are then far from fp16's subnormal
-// numbers, in which a second half would lose its bits.  Where a scale of 2 or
-// more has been seen the range is 2^0 .. 2^2, since 2^2 times the largest scale
-// (2 * 65504 / 15) is the most that fp16 takes.
-constexpr float kHigh = 10.0f, kHighSet = 8.0f, kLow = 2.0f, kLowSet = 0.0f;
+// What a probability times a value scale is held in.  The running reference
+// of a row (log2) is kept so that its largest probability so far lies in 2^12 ..
+// 2^14, and a unit of each group, a power of two, so that the largest scale seen
+// lies in 1 .. 2 units: the product is below 2^15, which fp16 takes, and what
+// two halves leave out is 2^-21 of it or, rounded, 2^-25, which is 2^-37 of the
+// largest probability times the largest scale.  (One unit for all groups would
+// cost an ordinary group the bits that an outlier in another one needs, and a
+// fixed one those of small scales.)  The reference holds the unit of group 0 as
+// well, whose products need no multiplication for it then.
+constexpr float kHigh = 14.0f, kHighSet = 12.0f;
 
 __device__ inline half2v pair(uint32_t b) { return __builtin_bit_cast(half2v, b); }
+
+// The pair with the largest scale, in its low half; as whole numbers, which have
+// the order of the scales (NaN is the largest).  The upper half may be anything.
+__device__ inline uint32_t larger(uint32_t a, uint32_t b) {
+  typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
+}
+// Of three at a time, four instructions for eight in place of seven, which heads
+// of 256 have no registers for.
+template <int D>
+__device__ inline uint32_t largest(uint32_t a, uint32_t b, uint32_t c) {
+  if constexpr (D == 256) return larger(larger(a, b), c);
+  uint32_t d;
+  asm("v_max3_u16 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+
+// f over the four lanes that hold a row's tokens (16 lanes apart), in each of them.
+template <class F>
+__device__ inline uint32_t over_row(uint32_t x, F f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return f(b[0], b[1]);
+}
 
 // Two fp32 numbers as fp16 rounded towards 0, and what that left.
 __device__ inline uint32_t cut(float a, float b) {
@@ -88,6 +117,13 @@ __device__ inline float rest1(uint32_t h, float w) {
   asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(h), "v"(w));
   return d;
 }
+
+// For x in 2^e .. 2^(e + 1): 2^e, 2^-e and e.
+__device__ inline float power_of(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0x7F800000u); }
+__device__ inline float over_power(float x) {
+  return __builtin_bit_cast(float, 0x7F000000u - (__builtin_bit_cast(uint32_t, x) & 0x7F800000u));
+}
+__device__ inline float log2_of(float x) { return (float)((int)(__builtin_bit_cast(uint32_t, x) >> 23) - 127); }
 
 struct Args {
   const uint8_t* layer;    // the layer's pages
@@ -418,15 +454,23 @@ kv_attn_kernel(Args args) {
   const float kNone = -3.0e38f;
   float4v acc[VD];
   float macc[NG], ref, grow, l;
-  bool low;   // the row has seen a large value scale
+  // Twice the unit of group 0 (a power of two that ref holds: its logarithm is
+  // added), and that unit over the other groups'.  At first the smallest scale
+  // there is.
+  float unit2 = 0x1p-23f, per_unit[NG];
   ref = 0.0f;
-  low = false;
   grow = kNone;
   l = 0.0f;
 #pragma unroll
-  for (int g = 0; g < NG; ++g) macc[g] = 0.0f;
+  for (int g = 0; g < NG; ++g) {
+    macc[g] = 0.0f;
+    per_unit[g] = 1.0f;
+  }
 #pragma unroll
   for (int j = 0; j < VD; ++j) acc[j] = float4v{0, 0, 0, 0};
+  // Some row of the wave has sums that are not 0 (or are NaN): what its first
+  // record brings has nothing to rescale.  (Heads of 256 would spill.)
+  auto begun = [&] { return D == 256 || __builtin_amdgcn_ballot_w64(l != 0.0f) != 0; };
   auto rescale = [&](float f) {
     l *= f;
 #pragma unroll
@@ -447,13 +491,6 @@ kv_attn_kernel(Args args) {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int j = 0; j < KD; ++j) kf[h][j] = code_operand(r.k[h][j]);
-    uint32_t scales = 0;
-#pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) scales |= r.vp[g][h][i];
     u4v hi[NG], lo[NG];
     float s[2][4];
 #pragma unroll
@@ -480,9 +517,7 @@ kv_attn_kernel(Args args) {
     for (int g = 0; g < NG; ++g)
 #pragma unroll
       for (int h = 0; h < 2; ++h) vp[g][h] = r.vp[g][h];
-    uint32_t any = scales;
     if (!whole) {
-      any = 0;
       asm volatile("");   // a branch: as selects the masks cost every record 40 instructions
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -492,44 +527,67 @@ kv_attn_kernel(Args args) {
           const bool see = tok <= pos && (a.window <= 0 || tok > pos - a.window);
           if (!see) s[h][i] = -__builtin_inff();
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            vp[g][h][i] = see ? vp[g][h][i] : 0u;   // may be anything
-            any |= vp[g][h][i];
-          }
+          for (int g = 0; g < NG; ++g) vp[g][h][i] = see ? vp[g][h][i] : 0u;   // may be anything
         }
-    }
-    // A row's first value scale of 2 or more (or NaN) among the tokens it sees.
-    if (__builtin_amdgcn_ballot_w64((any & 0x4000u) != 0 && !low) != 0) {
-      any |= __shfl_xor(any, 16);
-      any |= __shfl_xor(any, 32);
-      if ((any & 0x4000u) != 0 && !low) {
-        low = true;
-        if (grow != kNone) {
-          ref += kHigh - kLow;
-          grow = kLow;
-          rescale(exp2f(kLow - kHigh));
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[h][i] -= kHigh - kLow;
-        }
-      }
     }
     float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                       fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     if (__builtin_amdgcn_ballot_w64(top > grow) != 0) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = __builtin_bit_cast(float, over_row(__builtin_bit_cast(uint32_t, top), [](uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+      }));
+      const bool some = begun();
       if (top > grow) {
-        const float by = top - (low ? kLowSet : kHighSet);
+        const float set = kHighSet - log2_of(0.5f * unit2), by = top - set;
+        if (some) rescale(grow == kNone ? 0.0f : exp2f(-by));
         ref += by;
-        rescale(grow == kNone ? 0.0f : exp2f(-by));
-        grow = low ? kLow : kHigh;
+        grow = set + (kHigh - kHighSet);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[h][i] -= by;
       }
+    }
+    // The largest scale of a group among the tokens that the row sees.  (NaN, as
+    // a number the largest there is, makes no unit larger.)
+    uint32_t most[NG];
+    float big = 0.0f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const u4v x = vp[g][0], y = vp[g][1];
+      most[g] = larger(largest<D>(largest<D>(x[0], x[1], x[2]), x[3], y[0]), largest<D>(y[1], y[2], y[3]));
+      big = fmaxf(big, fmaf(lo_half(most[g]), per_unit[g], 0.0f));
+    }
+    if (__builtin_amdgcn_ballot_w64(big >= unit2) != 0) {
+      const float unit0 = 0.5f * unit2;
+      const bool some = begun();
+      float now0 = unit0;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const uint32_t x = over_row(most[g], larger);
+        const float unit = unit0 * over_power(per_unit[g]), scale = lo_half(x);
+        const float now = scale >= 2.0f * unit ? power_of(scale) : unit;
+        if (g == 0) now0 = now;
+        per_unit[g] = now0 * over_power(now);
+        const float f = unit * over_power(now);
+        if (some)
+#pragma unroll
+          for (int j = g * G / 16; j < (g + 1) * G / 16; ++j) acc[j] *= f;
+      }
+      // The reference and what is counted in it, for group 0.
+      const float f = unit0 * over_power(now0), by = -log2_of(f);
+      unit2 = 2.0f * now0;
+      if (some) {
+        l *= f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) macc[g] *= f;
+      }
+      ref += by;
+      grow -= by;   // kNone stays what it is
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[h][i] -= by;
     }
     float p[2][4];
 #pragma unroll
@@ -548,7 +606,9 @@ kv_attn_kernel(Args args) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const half2v v = pair(vp[g][h][i]);
-          w[h] = fmaf(p[h][i], (float)v[0], 0.0f);   // one instruction with the fp16 operand as it is
+          // One instruction with the fp16 operand as it is.  2^-25, half of what
+          // the second half can hold, makes the cut to it a rounding.
+          w[h] = fmaf(g == 0 ? p[h][i] : p[h][i] * per_unit[g], (float)v[0], 0x1p-25f);
           macc[g] = fmaf(p[h][i], fmaf(8.0f, (float)v[0], (float)v[1]), macc[g]);
         }
         const uint32_t x = cut(w[0], w[1]);
@@ -600,8 +660,9 @@ kv_attn_kernel(Args args) {
 #pragma unroll
   for (int j = 0; j < VD; ++j) {
     float4v y;
+    const float unit = kCodeUnit / per_unit[j * 16 / G];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = fmaf(acc[j][i], kCodeUnit, M[j * 16 / G]) * f;
+    for (int i = 0; i < 4; ++i) y[i] = fmaf(acc[j][i], unit, M[j * 16 / G]) * f;
     if (t.row0 + ocol < t.rows) *reinterpret_cast<float4v*>(&so[wave][ocol][16 * j + 4 * oc]) = y;
   }
   __syncthreads();
