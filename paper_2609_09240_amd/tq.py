@@ -841,11 +841,19 @@ def _kv_rows(t, heads, d, name):
     return TqKvRows(t.data_ptr(), t.stride(0), t.stride(1))
 
 
-def tq_kv_append(cache, layer, k, v, starts, seqs=None, cu_new=None, max_new=1, d_err=None, stream=None):
+def _most(given, cu, n_tokens):
+    """Tokens of a row at most, as the caller says or as there can be."""
+    return given if given is not None else (n_tokens if cu is not None else 1)
+
+
+def tq_kv_append(cache, layer, k, v, starts, seqs=None, cu_new=None, max_new=None, d_err=None, stream=None):
     """Quantise keys and values k, v [T, n_kv_heads, D] into the cache at the
     positions that tq_kv_extend gave (starts); row i's tokens are cu_new[i] ..
-    cu_new[i + 1] - 1 (token i without cu_new), at most max_new a row."""
+    cu_new[i + 1] - 1 (token i without cu_new).  max_new: what no row has more
+    of; tokens past it are left out.  Without it as many as there are tokens,
+    which is right and starts more workgroups than a number that fits."""
     n = starts.numel()
+    max_new = _most(max_new, cu_new, k.shape[0])
     if k.shape != v.shape:
         raise ValueError("k and v must have the same shape")
     kr = _kv_rows(k, cache.n_kv_heads, cache.head_dim, "k")
@@ -856,10 +864,12 @@ def tq_kv_append(cache, layer, k, v, starts, seqs=None, cu_new=None, max_new=1, 
     _used_on(stream, k, v, starts, seqs, cu_new, d_err, *cache._buffers())
 
 
-def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=1, k=None, v=None, stream=None):
-    """fp16 keys and values [n_tokens, n_kv_heads, D] of cached tokens; rows
-    and positions as in tq_kv_append."""
+def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=None, k=None, v=None, stream=None):
+    """fp16 keys and values [n_tokens, n_kv_heads, D] of cached tokens; rows,
+    positions and max_new as in tq_kv_append.  Tokens that no row has are not
+    written."""
     n = starts.numel()
+    max_new = _most(max_new, cu_new, n_tokens)
     shape = (n_tokens, cache.n_kv_heads, cache.head_dim)
     if k is None:
         k = torch.empty(shape, dtype=torch.float16, device=cache.lens.device)
@@ -874,17 +884,21 @@ def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=1
     return k, v
 
 
-def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=1, max_len=0, scale=None, window=0, o=None,
+def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0, scale=None, window=0, o=None,
                     lse=None, out_f32=False, want_lse=False, workspace=None, stream=None):
     """Attention of q [T, n_heads, D], the last tokens of their slots, over the
     cache: o [T, n_heads, D] (fp16 or fp32), and with want_lse also the log of
-    the softmax's sum, fp32 [T, n_heads].  scale: 1 / sqrt(D) without.  A
+    the softmax's sum, fp32 [T, n_heads].  scale: 1 / sqrt(D) without.  max_q:
+    what no row has more queries of (the tokens past it are not computed);
+    without it as many as there are tokens, which is right and may be slower
+    than a number that fits.  Tokens that no row has are not written.  A
     workspace of the caller's has zeros in its first WORKSPACE_COUNT_BYTES
     before its first call."""
     T, n_heads, D = q.shape
     n = seqs.numel() if seqs is not None else (cu_q.numel() - 1 if cu_q is not None else T)
     if cu_q is None and n != T:
         raise ValueError("without cu_q, q must have one token a row")
+    max_q = _most(max_q, cu_q, T)
     qr = _kv_rows(q, None, cache.head_dim, "q")
     dtype = torch.float32 if out_f32 else torch.float16
     if o is None:
