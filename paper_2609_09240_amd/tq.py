@@ -841,6 +841,13 @@ def _kv_rows(t, heads, d, name):
     return TqKvRows(t.data_ptr(), t.stride(0), t.stride(1))
 
 
+def _fits(*numbers):
+    """Numbers that are passed as 32 bits; ctypes would cut them without a word."""
+    for x in numbers:
+        if x >> 31 not in (0, -1):
+            raise ValueError(f"{x} does not fit 32 bits")
+
+
 def _most(given, cu, n_tokens):
     """Tokens of a row at most, as the caller says or as there can be."""
     return given if given is not None else (n_tokens if cu is not None else 1)
@@ -854,6 +861,7 @@ def tq_kv_append(cache, layer, k, v, starts, seqs=None, cu_new=None, max_new=Non
     which is right and starts more workgroups than a number that fits."""
     n = starts.numel()
     max_new = _most(max_new, cu_new, k.shape[0])
+    _fits(layer, max_new)
     if k.shape != v.shape:
         raise ValueError("k and v must have the same shape")
     kr = _kv_rows(k, cache.n_kv_heads, cache.head_dim, "k")
@@ -870,6 +878,7 @@ def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=N
     written."""
     n = starts.numel()
     max_new = _most(max_new, cu_new, n_tokens)
+    _fits(layer, max_new, n_tokens)
     shape = (n_tokens, cache.n_kv_heads, cache.head_dim)
     if k is None:
         k = torch.empty(shape, dtype=torch.float16, device=cache.lens.device)
@@ -899,6 +908,7 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
     if cu_q is None and n != T:
         raise ValueError("without cu_q, q must have one token a row")
     max_q = _most(max_q, cu_q, T)
+    _fits(layer, max_q, max_len, window)
     qr = _kv_rows(q, None, cache.head_dim, "q")
     dtype = torch.float32 if out_f32 else torch.float16
     if o is None:
