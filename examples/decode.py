@@ -136,7 +136,7 @@ def generate(layers=2, branches=3, tokens=24, seed=0, log=print):
 
     # One row from here on: the step as a graph, its token and logits in place.
     seq, tok, kept = kids[keep:keep + 1].clone(), nxt[keep:keep + 1].clone(), out[keep]
-    ws = m.cache.attention_workspace(4 << 20)
+    ws = m.cache.attention_workspace(tq.tq_kv_attention_workspace_bytes(m.cache, 1, m.heads, max_len=m.max_len))
     left = tokens - tokens // 2
     # (A first step outside of the graph; it counts.)
     tok.copy_(m.step(tok, seq, workspace=ws).argmax(-1))

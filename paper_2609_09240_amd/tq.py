@@ -893,6 +893,16 @@ def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=N
     return k, v
 
 
+def tq_kv_attention_workspace_bytes(cache, n_rows, n_heads, n_tokens=None, max_q=1, max_len=0, window=0):
+    """Workspace of tq_kv_attention for n_rows rows of n_tokens queries together
+    (max_q a row without), 0 where it uses none."""
+    T = n_rows * max_q if n_tokens is None else n_tokens
+    _fits(n_rows, T, max_q, n_heads, max_len, window)
+    # (Slots that are not read here: more rows than slots are allowed where rows name theirs.)
+    a = TqKvAttn(n_rows, T, max_q, n_heads, max_len, window, 1.0, OUT_FP16, cache.lens.data_ptr())
+    return int(lib().tq_kv_attention_workspace_bytes(cache._ref, a))
+
+
 def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0, scale=None, window=0, o=None,
                     lse=None, out_f32=False, want_lse=False, workspace=None, stream=None):
     """Attention of q [T, n_heads, D], the last tokens of their slots, over the

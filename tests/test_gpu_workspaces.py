@@ -102,3 +102,20 @@ def test_one_workspace_for_products_and_attention():
         tq.tq_kv_attention(m.cache, 0, q, o=got_o, workspace=ws)
         assert torch.equal(got_y, y) and torch.equal(got_o, o)
         assert bool((ws[:tq.WORKSPACE_COUNT_BYTES] == 0).all())
+
+
+@pytest.mark.parametrize("nq,max_len,window", [([1, 1], 0, 0), ([1, 1], 3000, 0), ([9, 2], 2000, 700), ([1, 1], 100, 0)])
+def test_attention_workspace_bytes(nq, max_len, window):
+    """What the size says is enough, and less is refused."""
+    m = Model([3000, 40], 2, 128, 64, 64)
+    q = torch.from_numpy(rows((sum(nq), 8, 128), 1)).cuda()
+    cu = torch.tensor([0, *np.cumsum(nq).tolist()], dtype=torch.int32, device="cuda")
+    kw = dict(cu_q=cu, max_q=max(nq), max_len=max_len, window=window)
+    need = tq.tq_kv_attention_workspace_bytes(m.cache, 2, 8, sum(nq), max(nq), max_len, window)
+    want = tq.tq_kv_attention(m.cache, 0, q, **kw)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    assert torch.equal(tq.tq_kv_attention(m.cache, 0, q, workspace=ws, **kw), want)
+    assert (need == 0) == (max_len == 100)
+    if need:
+        with pytest.raises(tq.TqError):
+            tq.tq_kv_attention(m.cache, 0, q, workspace=ws[:need - 16].clone(), **kw)
