@@ -240,9 +240,9 @@ __device__ inline float4v sum_waves(const float4v (*part)[S][64], int i, int l) 
 
 // Few rows of X: every wave reads the inputs of its block from memory in the
 // shape of the operand (16 bytes of up to four rows, 64 bytes apart from each
-// other's lanes).  A wave takes the blocks wave, wave + W, ... of RT row tiles,
-// NB of them in its registers or on their way.
-template <int G, int RT, int W, int NB>
+// other's lanes).  A wave takes the blocks wave, wave + W, ... of RT row tiles;
+// the next one is on its way as registers become free.
+template <int G, int RT, int W>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) q4_gemv_kernel(const uint8_t* __restrict__ codes,
                                                          const uint32_t* __restrict__ params,
                                                          const uint16_t* __restrict__ X, int64_t ldx, int N, int K,
@@ -265,36 +265,35 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) acc[rt][0] = float4v{0, 0, 0, 0};
 
-  u4v w[NB][RT];
-  uint32_t p[NB][RT];
-  half8 x[NB][1][4];
-  auto load_w = [&](int s, int rt, int blk) {
-    w[s][rt] = wp[rt][(int64_t)blk * 64];
-    p[s][rt] = pp[rt][(int64_t)blk * NG * 16];
+  u4v w[RT];
+  uint32_t p[RT];
+  half8 x[1][4];
+  auto load_w = [&](int rt, int blk) {
+    w[rt] = wp[rt][(int64_t)blk * 64];
+    p[rt] = pp[rt][(int64_t)blk * NG * 16];
   };
-  auto load_x = [&](int s, int blk) {
+  auto load_x = [&](int blk) {
     if (blk * 128 + 128 <= K) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[s][0][j] = load8(xp + blk * 128 + 32 * j + 8 * c);
+      for (int j = 0; j < 4; ++j) x[0][j] = load8(xp + blk * 128 + 32 * j + 8 * c);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[s][0][j] = load_tail(xp, blk * 128 + 32 * j + 8 * c, K);
+      for (int j = 0; j < 4; ++j) x[0][j] = load_tail(xp, blk * 128 + 32 * j + 8 * c, K);
     }
   };
+  // Past the last block the last is read again and not used.
 #pragma unroll
-  for (int s = 0; s < NB; ++s) {
-    const int blk = min(wave + s * W, KB - 1);   // past the last block: read again, not used
+  for (int rt = 0; rt < RT; ++rt) load_w(rt, min(wave, KB - 1));
+  load_x(min(wave, KB - 1));
+  for (int blk = wave; blk < KB; blk += W) {
+    const int next = min(blk + W, KB - 1);
+    // (As a loop of one pass: without it the compiler takes 169 registers where it
+    // took 167, and a SIMD holds two waves in place of three.  131072 x 4096 at B =
+    // 1, groups of 64: 58.9 us and 53.5.)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) load_w(s, rt, blk);
-    load_x(s, blk);
-  }
-  for (int blk0 = wave; blk0 < KB; blk0 += NB * W) {
-#pragma unroll
-    for (int s = 0; s < NB; ++s) {
-      if (blk0 + s * W >= KB) break;
-      const int next = min(blk0 + (NB + s) * W, KB - 1);
-      block_product<G, RT, 1>(w[s], p[s], x[s], acc, [&](int rt) { load_w(s, rt, next); });
-      load_x(s, next);
+    for (int once = 0; once < 1; ++once) {
+      block_product<G, RT, 1>(w, p, x, acc, [&](int rt) { load_w(rt, next); });
+      load_x(next);
     }
   }
   __shared__ float4v part[W][RT][64];
@@ -340,9 +339,8 @@ __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __
   }
 
   // Thread i of the workgroup brings 8 inputs of kLoads rows, of two chunks in
-  // turn where the registers allow.
-  constexpr int kIn = kLoads <= 8 ? 2 : 1;
-  half8 in[kIn][kLoads];
+  // turn.
+  half8 in[2][kLoads];
   auto fetch = [&](int s, int chunk) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -372,7 +370,7 @@ __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) load_w(0, rt, first);
     fetch(0, first);
-    if (kIn == 2 && first + 1 < chunks) fetch(1, first + 1);
+    if (first + 1 < chunks) fetch(1, first + 1);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) load_w(1, rt, first + 1);
     stage(0, 0);
@@ -384,7 +382,7 @@ __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __
       const int chunk = chunk0 + s;
       if (chunk >= chunks) break;
       const bool more = chunk + 1 < chunks;
-      if (chunk + kIn < chunks) fetch(kIn == 2 ? s : 0, chunk + kIn);
+      if (chunk + 2 < chunks) fetch(s, chunk + 2);
       half8 x[CT][4];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
@@ -393,7 +391,7 @@ __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __
           x[ct][j] = *reinterpret_cast<const half8*>(&lds[(s * 16 * CT + 16 * ct + col) * kRow + wk * 128 + 32 * j + 8 * c]);
       // Blocks past the last one meet inputs of 0 only.
       block_product<G, RT, CT>(w[s], p[s], x, acc, [&](int rt) { load_w(s, rt, chunk + 2); });
-      if (more) stage(kIn == 2 ? s ^ 1 : 0, s ^ 1);
+      if (more) stage(s ^ 1, s ^ 1);
       __syncthreads();
     }
   }
@@ -434,10 +432,10 @@ __global__ void __launch_bounds__(64 * WK * WR) q4_gemm_kernel(const uint8_t* __
   }
 }
 
-template <int G, int RT, int W, int NB>
+template <int G, int RT, int W>
 void start_gemv(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* Y, bool out_f32, hipStream_t s) {
   const int NT = (m.n_out + 15) / 16;
-  q4_gemv_kernel<G, RT, W, NB><<<(NT + RT - 1) / RT, 64 * W, 0, s>>>(
+  q4_gemv_kernel<G, RT, W><<<(NT + RT - 1) / RT, 64 * W, 0, s>>>(
       m.codes, reinterpret_cast<const uint32_t*>(m.params), X, ldx, m.n_out, m.n_in, B, Y, out_f32 ? 1 : 0);
 }
 
@@ -506,11 +504,11 @@ hipError_t start_g(const Q4Dev& m, const uint16_t* X, int64_t ldx, int B, void* 
   const bool wide = NT > 512;
   if (B <= 2 || (B <= 4 && !wide)) {
     if (NT >= 2048)
-      start_gemv<G, 4, 4, 1>(m, X, ldx, B, Y, out_f32, s);
+      start_gemv<G, 4, 4>(m, X, ldx, B, Y, out_f32, s);
     else if (wide)
-      start_gemv<G, 2, 4, 1>(m, X, ldx, B, Y, out_f32, s);
+      start_gemv<G, 2, 4>(m, X, ldx, B, Y, out_f32, s);
     else
-      start_gemv<G, 1, 8, 1>(m, X, ldx, B, Y, out_f32, s);
+      start_gemv<G, 1, 8>(m, X, ldx, B, Y, out_f32, s);
     return hipSuccess;
   }
   if (B <= 16)
