@@ -1,9 +1,9 @@
 // Attention over the 4-bit paged cache (gfx950), one pass over the keys and
 // values with the running maximum and sum of the softmax:
-//     s_j = scale * sum_g ( sk_jg (q . ck_j)_g + mk_jg sum_g q )
-//     o   = sum_j ( p_j sv_jg ) cv_j  +  sum_j p_j mv_jg,   p_j = exp(s_j - max) / sum
-// ck, cv: the codes less 8; sk, mk, sv, mv: scale and centred offset of token
-// j's group g of channels.  No key or value is formed: the codes are exact
+//     s_j = scale * sum_g ( sk_jg ((q . ck_j)_g + 8 sum_g q) + mk_jg sum_g q )
+//     o   = sum_j ( p_j sv_jg ) cv_j  +  sum_j p_j (mv_jg + 8 sv_jg),   p_j = exp(s_j - max) / sum
+// ck, cv: the codes less 8; sk, mk, sv, mv: scale and offset of token j's group
+// g of channels.  No key or value is formed: the codes are exact
 // operands of the matrix instructions and the parameters multiply the fp32
 // sums (keys) or the probabilities (values).
 //
@@ -15,7 +15,7 @@
 //   with those eight tokens in one word: O^T += V^T P^T.
 // A probability times a value scale enters as two fp16 numbers (hi + lo, 22
 // bits), in a unit of the row and group that follows the largest scale seen;
-// the sums of p, of p mv and of everything else are fp32.
+// the sums of p, of p (mv + 8 sv) and of everything else are fp32.
 //
 // Work split: a workgroup has four waves that take the records of its range
 // in turn and join their references, sums and outputs through LDS.  Where there
@@ -274,8 +274,9 @@ struct Record {
 };
 
 // The kernel's arguments read anew: what a stretch of code needs of them holds
-// no scalar registers outside of it.  (All of them kept through the kernel,
-// with the state of the shares, spill 70 scalar registers.)
+// no scalar registers outside of it.  (41 to 52 of those live in lanes of vector
+// registers meanwhile; with all arguments kept, 111 to 127, and some variants
+// spill vector registers for them.)
 __device__ inline Args args_anew() {
   typedef const __attribute__((address_space(4))) Args* ptr;
   ptr p = (ptr)__builtin_amdgcn_kernarg_segment_ptr();
@@ -283,8 +284,8 @@ __device__ inline Args args_anew() {
   return *(const Args*)p;
 }
 
-// Waves a SIMD holds of a variant, as many as its registers allow without a
-// spill (512 / waves of them; past 256 half of them are accumulation registers
+// Waves a SIMD holds of a variant, as many as its vector registers allow without
+// a spill (512 / waves of them; past 256 half of them are accumulation registers
 // that cost moves).
 constexpr int waves_of(int D, int G) { return D == 64 ? 4 : D == 128 ? (G == 32 ? 2 : 3) : 1; }
 

@@ -93,11 +93,15 @@ __device__ inline half8 load8(const uint16_t* p) { return reinterpret_cast<const
 // a code, masked, are the subnormal number n * 2^-24 (n * 2^-20 where they sit
 // 4 bits up); one exact multiply-add makes it normal and centred: 9
 // instructions for 8 codes, and kCodeUnit is left to the fp32 sums.
-// Around 0, because a sum of codes and the sum that its offset multiplies
-// cancel where the values do: with offset + 8 scale in the place of the offset
-// both are small.  Normal, because the matrix cores align operands by their
-// exponent alone: subnormal ones, which would save the multiply-add, lose 7
-// bits of the sum (measured: 7.6e-6 off where a product is now 1.3e-7 off).
+// Around 0, which costs nothing: cached values are summed so, with offset +
+// 8 scale in the place of the offset, and both sums are small where the values
+// are; products and keys start the sum of their codes at 8 times that of the
+// other operand, and multiply the offset as it is.
+// Normal, because the matrix cores align products by their operands' exponents
+// alone: subnormal codes, which would save the multiply-add, lose 7 bits of the
+// sum (measured: 7.6e-6 off where a product is now 1.3e-7 off).  The other
+// operand may be subnormal: its bits lie within ten below 2^-14, and with four
+// of a code that is less than the sum holds (measured: 1e-7 off or less).
 constexpr float kCodeUnit = 512.0f;
 __device__ inline half8 code_operand(uint32_t w) {
   const half2v a = {(_Float16)32768.0f, (_Float16)32768.0f}, b = {(_Float16)2048.0f, (_Float16)2048.0f};
@@ -143,9 +147,6 @@ __device__ __forceinline__ uint32_t row_bcast(uint32_t x, int n) {
   }
 }
 #undef TQ_ROW_BCAST
-
-// The offset that goes with codes around 0.
-__device__ inline float centred(float s, float m) { return fmaf(8.0f, s, m); }
 
 // Nibble of element e of eight, and eight codes as a word.
 __device__ inline constexpr int nibble_of(int e) { return (e & 1) * 4 + (e >> 1); }
