@@ -841,11 +841,12 @@ def _kv_rows(t, heads, d, name):
     return TqKvRows(t.data_ptr(), t.stride(0), t.stride(1))
 
 
-def _fits(*numbers):
-    """Numbers that are passed as 32 bits; ctypes would cut them without a word."""
-    for x in numbers:
-        if x >> 31 not in (0, -1):
-            raise ValueError(f"{x} does not fit 32 bits")
+def _fits(bits):
+    """Numbers that are passed as 32 bits, or'ed together: ctypes would cut those
+    that do not fit without a word.  Where one of them hides behind a negative
+    one, a number with bit 31 set is passed, which the library refuses."""
+    if bits >> 31 not in (0, -1):
+        raise ValueError("a number does not fit 32 bits")
 
 
 def _most(given, cu, n_tokens):
@@ -861,7 +862,7 @@ def tq_kv_append(cache, layer, k, v, starts, seqs=None, cu_new=None, max_new=Non
     which is right and starts more workgroups than a number that fits."""
     n = starts.numel()
     max_new = _most(max_new, cu_new, k.shape[0])
-    _fits(layer, max_new)
+    _fits(layer | max_new)
     if k.shape != v.shape:
         raise ValueError("k and v must have the same shape")
     kr = _kv_rows(k, cache.n_kv_heads, cache.head_dim, "k")
@@ -878,7 +879,7 @@ def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=N
     written."""
     n = starts.numel()
     max_new = _most(max_new, cu_new, n_tokens)
-    _fits(layer, max_new, n_tokens)
+    _fits(layer | max_new | n_tokens)
     shape = (n_tokens, cache.n_kv_heads, cache.head_dim)
     if k is None:
         k = torch.empty(shape, dtype=torch.float16, device=cache.lens.device)
@@ -897,7 +898,7 @@ def tq_kv_attention_workspace_bytes(cache, n_rows, n_heads, n_tokens=None, max_q
     """Workspace of tq_kv_attention for n_rows rows of n_tokens queries together
     (max_q a row without), 0 where it uses none."""
     T = n_rows * max_q if n_tokens is None else n_tokens
-    _fits(n_rows, T, max_q, n_heads, max_len, window)
+    _fits(n_rows | T | max_q | n_heads | max_len | window)
     # (Slots that are not read here: more rows than slots are allowed where rows name theirs.)
     a = TqKvAttn(n_rows, T, max_q, n_heads, max_len, window, 1.0, OUT_FP16, cache.lens.data_ptr())
     return int(lib().tq_kv_attention_workspace_bytes(cache._ref, a))
@@ -918,7 +919,7 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
     if cu_q is None and n != T:
         raise ValueError("without cu_q, q must have one token a row")
     max_q = _most(max_q, cu_q, T)
-    _fits(layer, max_q, max_len, window)
+    _fits(layer | max_q | max_len | window)
     qr = _kv_rows(q, None, cache.head_dim, "q")
     dtype = torch.float32 if out_f32 else torch.float16
     if o is None:
