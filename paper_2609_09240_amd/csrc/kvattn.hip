@@ -22,23 +22,28 @@
 // are few tiles over long caches the records of all of them are laid in a
 // line and divided evenly among as many workgroups as the chip holds, whatever
 // the lengths are; a tile that several workgroups have parts of is joined by
-// the last of them to finish.  Otherwise a workgroup has a tile.
+// the last of them to finish.  Otherwise a workgroup has a tile: also where there
+// are more than 256 tiles and rows, one of them over a long cache or not (300
+// rows, one of them 131072 tokens long: 1036 us; 200: 69).
 //
 // A record's 4.6 KB (D = 128, groups of 64) arrive in the registers of the
 // record before, each as soon as it is used; 168 of them allow three waves a
 // SIMD.  One token over one long cache: 5.4 TB/s for every further byte, and
 // 6 us of launch, table, first loads and joining waves before the first, 7 us
 // for joining 96 parts a head.
-//   1 x 131072 tokens, 8 heads, groups of 128 (143 MB)  40.3 us
-//   32 ragged rows to 8192, groups of 64 (93 MB)        33.2
-//   1 x 4096 (4.7 MB)                                   11.8
+//   1 x 131072 tokens, 8 heads, groups of 128 (143 MB)  40.2 us
+//   32 ragged rows to 8192, groups of 64 (93 MB)        34.3
+//   1 x 4096 (4.7 MB)                                   12.0
 //   1 x 45                                              6.4
+//   8 x 8 queries of ragged rows to 8192 (31 MB)        34.6
 //   a chunk of 2 x 1000 queries over up to 5000, window 2048, 14 heads of 64 on
-//   2, groups of 32 (10 GFLOP)                          77
+//   2, groups of 32 (10 GFLOP)                          82
+// A unit a group cost 1 to 5 % of these (the largest scale of a record, and a
+// multiplication a probability and group behind the first).
 // (One launch a split and another to join: 31 + 6.5, 33 + 6 and 10 + 6 for the
 // first three, and 3 us between the launches.  32 or 64 rows a tile, which
 // unpack a record once for two or four tiles, halve the waves: 90 and 120 us
-// for the chunk, 37 where 8 queries of 4 heads take 29.)
+// where the chunk took 77, 37 where 8 queries of 4 heads took 29.)
 
 #include "q4_internal.h"
 

@@ -6,11 +6,14 @@
 // of theirs holds 8 tokens of one channel.  A word that also holds tokens
 // that are not new is read, changed and written back by one thread.
 //
-// 6000 tokens of 8 heads of 128 in groups of 32 (24.6 MB in, 7.7 MB out): 15.0
-// us, 2.1 TB/s (13.5 at best), bound by the arithmetic of the codes, which takes
-// 59 % of the vector slots (a division a value took 1.5 times as long); read
-// back 13.4 us, 2.4 TB/s, 47 % of them.  One token each of 64 rows: 5.6 and 4.1
-// us, the launch and three trips to memory one after the other.
+// 6000 tokens of 8 heads of 128 in groups of 32 (24.6 MB in, 7.7 MB out): 14.9
+// us, 2.2 TB/s (13.8 at best), read back 13.2 us, 2.4 TB/s.  Neither is at a
+// bound: the copy rate is 4.9 TB/s, the arithmetic takes 59 and 48 % of the
+// vector slots (a division a value took 1.5 times as long).  What is left in the
+// code: value words go out 16 bytes apart, and reading back divides by three
+// run-time numbers for every 8 channels and reads a word of LDS a value.  One
+// token each of 64 rows: 5.7 and 4.2 us, the launch and three trips to memory
+// one after the other.
 
 #include "q4_internal.h"
 

@@ -15,6 +15,10 @@
 // shared pages and the caches), 64 MB of a compaction read and written in 23.7,
 // 5.4 TB/s.  (1024 threads for any number of rows: 9.6
 // and 7.0 us; the free pages of a thread handed out one after the other: 11.6.)
+// Free pages are searched for from page 0 on, 4096 a pass, and a compaction's
+// plan walks the pool twice: room for 64 rows 7.2 us in a pool of 1000 pages
+// and 57 in one of 100000, 92 % of them in use, a compaction with nothing to
+// move 4.2 and 80.
 
 #include "q4_internal.h"
 
