@@ -23,9 +23,10 @@
 //   131072 x 4096   B = 1 52.7 (groups of 64: 302 MB, 5.7 TB/s), 16 76
 // B = 1 of a large matrix is bound by HBM, of a small one by latency; from B =
 // 16 on by X, which every workgroup reads: a workgroup of four row tiles at B =
-// 64 brings 16 times the bytes of X that it brings of codes, so where there are
-// few row groups each is split along K, and the parts are joined by the last of
-// them to finish.
+// 64, or of one at B = 16, brings four times the bytes of X that it brings of
+// codes (4096 x 12288: 135 and 127 MB from L2, counted, for 27 of weights).  From
+// B = 17 on, where there are few row groups, each is split along K, and the parts
+// are joined by the last of them to finish.
 
 #include <atomic>
 

@@ -2,6 +2,9 @@
 replaced: a captured call never gets, and never leaves behind, a buffer that
 an eager call uses, since a graph outlives the handle's hold on it."""
 
+import os
+import re
+
 import pytest
 import torch
 
@@ -66,3 +69,10 @@ def test_counts_are_zeros(streams, monkeypatch, need):
     for streams.capturing in (False, True):
         t = tq._Workspaces("cpu").get(need, None)
         assert bool((t[:tq.WORKSPACE_COUNT_BYTES] == 0).all())
+
+
+def test_the_header_says_the_same():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "tq.h")
+    with open(path) as f:
+        n = re.search(r"#define TQ_WORKSPACE_COUNT_BYTES (\d+)", f.read())
+    assert int(n.group(1)) == tq.WORKSPACE_COUNT_BYTES
