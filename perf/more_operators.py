@@ -356,7 +356,8 @@ def prepare(c, seed):
     st["cu"] = torch.arange(0, b * c["nq"] + 1, c["nq"], device="cuda", dtype=torch.int32)
     if c["kind"] == "shared":
         rows, prefix = _groups(c)
-        st["prefix"] = torch.tensor(prefix, dtype=torch.int32).cuda()
+        st["prefix"] = torch.tensor([p for r, p in zip(rows, prefix) for _ in range(r)], dtype=torch.int32).cuda()
+        st["shared"] = torch.tensor(prefix).cuda()
         st["groups"] = torch.tensor([0] + torch.tensor(rows).cumsum(0).tolist(), dtype=torch.int32).cuda()
         # row of the call -> group and place in it; the other way round, filled up with row 0
         n, m = c["groups"], max(rows)
@@ -492,7 +493,7 @@ def _plain_shared(st, c):
     share, b = c["hq"] // H, st["lens"].numel()
     n, m = st["row_at"].shape
     q = _plain_queries(st, c, b)
-    prefix = st["prefix"].long()
+    prefix = st["shared"]
     # What a group shares, once: the queries of all its rows beside each other.
     k, v = _plain_rows(st, c, st["pages"].long()[st["row_at"][:, 0], :c["prefix"] // ps])
     j = torch.arange(c["prefix"], device="cuda")
@@ -501,7 +502,7 @@ def _plain_shared(st, c):
     part = _plain_sums(qs, k, v, (j < prefix[:, None])[:, None, None])
     top1, l1, o1 = (x.view(n, H, m, share * nq, -1).transpose(1, 2)[st["group_of"], st["place_of"]] for x in part)
     # What every row has behind it.
-    first, lens = prefix[st["group_of"]][:, None], st["lens"].long()[:, None]
+    first, lens = st["prefix"].long()[:, None], st["lens"].long()[:, None]
     col = first // ps + torch.arange(_pages(c["tail"], ps), device="cuda")
     k, v = _plain_rows(st, c, st["pages"].long().gather(1, col.clamp(max=st["pages"].shape[1] - 1)))
     j = first + torch.arange(k.shape[2], device="cuda")
