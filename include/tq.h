@@ -599,6 +599,135 @@ typedef struct tq_kv_attn {
 size_t tq_kv_attention_workspace_bytes(const tq_kv_cache* cache, const tq_kv_attn* a);
 tq_status tq_kv_attention(const tq_kv_cache* cache, int32_t layer, const tq_kv_attn* a, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Attention with a wider or a shared view of the cache.
+ *
+ * sinks: the first tokens of a slot that every query sees beside its window:
+ *     query at p sees j <= p with j > p - window or j < sinks.
+ * Only those tokens and the windows are read.  Without a window (0) every
+ * token is seen, and sinks change nothing.
+ *
+ * prefix: rows whose slots name the same pages for their first tokens (the
+ * children of tq_kv_fork) are attended together over those: the shared
+ * tokens are read once a group for the queries of all its rows, and what
+ * every row has behind them is added.  The result is that of
+ * tq_kv_attention up to the order of the sums; sharing decides only the speed.
+ * Rows cu_rows[g] .. cu_rows[g + 1] - 1 are group g, cu_rows[0] = 0,
+ * cu_rows[n_groups] = n_rows, cu_q not decreasing.  prefix[i] is the number
+ * of first tokens that row i has in common with the other rows of its group,
+ * the same for all of them, or less than 32 for a row that shares nothing
+ * (only whole records of 32 tokens are shared).  tq_kv_shared_prefix finds
+ * these numbers.  Where they do not hold, the rows' results are unspecified;
+ * every access stays in bounds.  Rows with a window are attended one by one.
+ */
+typedef struct tq_kv_scope {
+  int32_t sinks;            /* >= 0 */
+  int32_t n_groups;         /* 0: no row shares anything; at most n_rows */
+  int32_t max_prefix;       /* longest prefix, and most tokens behind one, as far */
+  int32_t max_tail;         /* as the caller knows (0: max_len), for the split only */
+  const int32_t* cu_rows;   /* device int32 [n_groups + 1]; NULL: one group, n_groups = 1 */
+  const int32_t* prefix;    /* device int32 [n_rows] */
+} tq_kv_scope;
+
+size_t tq_kv_attention_scope_workspace_bytes(const tq_kv_cache* cache, const tq_kv_attn* a, const tq_kv_scope* scope);
+tq_status tq_kv_attention_scope(const tq_kv_cache* cache, int32_t layer, const tq_kv_attn* a,
+                                const tq_kv_scope* scope, void* stream);
+
+/* The tokens that rows of a group have in common: prefix[i] (device int32
+ * [n_rows]) becomes, for the rows of a group that hold tokens, those of the
+ * leading pages that all of them name alike, no more than the shortest of
+ * them holds; 0 for rows that hold none, whose slot is outside the cache,
+ * that are alone, or that no group has.  Once after the table changed, for
+ * all layers. */
+tq_status tq_kv_shared_prefix(const tq_kv_cache* cache, const int32_t* seqs, const int32_t* cu_rows,
+                              int32_t n_groups, int32_t n_rows, int32_t* prefix, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions of several axes (one for text; time, height and width
+ * for images and video), queries and keys in one call.
+ *
+ * Channel pair i < rot / 2 of a head is turned by the angle
+ *     positions[axis[i]][token] * freq[i]      (radians),
+ *     (x1, x2) -> scale * (x1 cos - x2 sin, x2 cos + x1 sin);
+ * its channels are i and i + rot/2, or 2i and 2i + 1 with TQ_ROPE_ADJACENT.
+ * Channels from rot on stay as they are.  TQ_ROPE_INVERSE turns the other way,
+ * which is also the gradient: that of x is the inverse call on that of the
+ * output.  Angles are reduced in 64 bits, at any position; products and sums
+ * are fp32, rounded once to fp16.
+ * In place (an output with the data and the strides of its input) or into
+ * memory that does not overlap any input. */
+#define TQ_ROPE_ADJACENT 1
+#define TQ_ROPE_INVERSE 2
+#define TQ_ROPE_MAX_DIM 1024
+#define TQ_ROPE_MAX_AXES 8
+#define TQ_ROPE_MAX_TOKENS ((1 << 24) - 1)
+#define TQ_ROPE_MAX_HEADS 65535
+
+typedef struct tq_out_rows {   /* as tq_kv_rows, written */
+  uint16_t* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} tq_out_rows;
+
+typedef struct tq_rope_call {
+  int32_t n_tokens;         /* 1 .. TQ_ROPE_MAX_TOKENS */
+  int32_t n_heads;          /* heads of q, 1 .. TQ_ROPE_MAX_HEADS */
+  int32_t n_kv_heads;       /* heads of k, as many at most; 0: no keys */
+  int32_t head_dim;         /* 2 .. TQ_ROPE_MAX_DIM */
+  int32_t rot;              /* even, 2 .. head_dim */
+  int32_t n_axes;           /* 1 .. TQ_ROPE_MAX_AXES */
+  int32_t flags;            /* TQ_ROPE_* or'ed */
+  float scale;              /* finite */
+  const int32_t* positions; /* device: token t on axis a at positions[a * axis_stride + t] */
+  int64_t axis_stride;
+  const float* freq;        /* device fp32 [rot / 2] */
+  const uint8_t* axis;      /* device [rot / 2]; NULL: axis 0.  A pair that names an
+                               axis which is not there is not turned, only scaled. */
+  tq_kv_rows q, k;          /* element d of head h of token t, 2-byte aligned */
+  tq_out_rows q_out, k_out;
+} tq_rope_call;
+
+tq_status tq_rope(const tq_rope_call* call, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Log probabilities of rows of logits: of given tokens, the entropy, and
+ * the most likely tokens, in one pass over the logits.
+ *     p_j = exp(scale x_j) / sum_i exp(scale x_i),  H = -sum_j p_j log p_j.
+ * Logits of -infinity (tokens that are ruled out) have the probability 0.  A
+ * row of nothing else has log probabilities of -infinity and the entropy 0.
+ * A NaN or +infinity in a row makes its log probabilities and entropy NaN.
+ * The most likely tokens are ordered by their logits, the larger one first, of
+ * equal ones (-0 equals +0) the lower index; a NaN ranks as -infinity.
+ * A given token outside 0 .. n_vocab - 1 gets NaN and counts in *d_err (device
+ * int32, may be NULL).  Sums are fp32.  Rows' results do not depend on the
+ * other rows' contents. */
+#define TQ_LOGITS_FP16 0
+#define TQ_LOGITS_FP32 1
+#define TQ_LOGPROBS_MAX_TOP 32
+#define TQ_LOGPROBS_MAX_IDS 1024
+
+typedef struct tq_logprobs_call {
+  int32_t n_rows;           /* 1 .. 2^20 */
+  int32_t n_vocab;          /* 1 .. 2^24 */
+  int32_t n_ids;            /* given tokens of a row, 0 .. TQ_LOGPROBS_MAX_IDS */
+  int32_t n_top;            /* most likely ones, 0 .. TQ_LOGPROBS_MAX_TOP, at most n_vocab */
+  int32_t flags;            /* TQ_LOGITS_FP16 or TQ_LOGITS_FP32 */
+  float scale;              /* finite, > 0 */
+  const void* logits;       /* rows ld >= n_vocab elements apart, aligned to an element */
+  int64_t ld;
+  const int32_t* ids;       /* device [n_rows][n_ids] */
+  float* logp;              /* [n_rows][n_ids] */
+  float* entropy;           /* [n_rows], may be NULL */
+  int32_t* top_ids;         /* [n_rows][n_top] */
+  float* top_logp;          /* [n_rows][n_top] */
+  int32_t* d_err;
+  void* workspace;          /* tq_logprobs_workspace_bytes, which may be 0; 16-byte */
+  size_t workspace_bytes;   /* aligned, its counts (TQ_WORKSPACE_COUNT_BYTES) zeros once */
+} tq_logprobs_call;
+
+size_t tq_logprobs_workspace_bytes(const tq_logprobs_call* call);
+tq_status tq_logprobs(const tq_logprobs_call* call, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,6 +26,11 @@ MAX_GROUPED = 8
 MAX_BATCH = 64
 Q4_MAX_BATCH = 64
 KV_MAX_ROWS = 1024
+ROPE_ADJACENT = 1
+ROPE_INVERSE = 2
+LOGITS_FP16 = 0
+LOGITS_FP32 = 1
+LOGPROBS_MAX_TOP = 32
 WORKSPACE_COUNT_BYTES = 16384   # at the front of a 4-bit operator's workspace
 
 STATUS = {0: "TQ_OK", 1: "TQ_ERR_NULL", 2: "TQ_ERR_SHAPE", 3: "TQ_ERR_ALIGN",
@@ -135,6 +140,59 @@ class TqKvAttn(ctypes.Structure):
     ]
 
 
+class TqKvScope(ctypes.Structure):
+    _fields_ = [
+        ("sinks", ctypes.c_int32),
+        ("n_groups", ctypes.c_int32),
+        ("max_prefix", ctypes.c_int32),
+        ("max_tail", ctypes.c_int32),
+        ("cu_rows", ctypes.c_void_p),
+        ("prefix", ctypes.c_void_p),
+    ]
+
+
+class TqRopeCall(ctypes.Structure):
+    _fields_ = [
+        ("n_tokens", ctypes.c_int32),
+        ("n_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rot", ctypes.c_int32),
+        ("n_axes", ctypes.c_int32),
+        ("flags", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("positions", ctypes.c_void_p),
+        ("axis_stride", ctypes.c_int64),
+        ("freq", ctypes.c_void_p),
+        ("axis", ctypes.c_void_p),
+        ("q", TqKvRows),
+        ("k", TqKvRows),
+        ("q_out", TqKvRows),       # tq_out_rows has the same members
+        ("k_out", TqKvRows),
+    ]
+
+
+class TqLogprobsCall(ctypes.Structure):
+    _fields_ = [
+        ("n_rows", ctypes.c_int32),
+        ("n_vocab", ctypes.c_int32),
+        ("n_ids", ctypes.c_int32),
+        ("n_top", ctypes.c_int32),
+        ("flags", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("logits", ctypes.c_void_p),
+        ("ld", ctypes.c_int64),
+        ("ids", ctypes.c_void_p),
+        ("logp", ctypes.c_void_p),
+        ("entropy", ctypes.c_void_p),
+        ("top_ids", ctypes.c_void_p),
+        ("top_logp", ctypes.c_void_p),
+        ("d_err", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -183,6 +241,13 @@ def lib():
             "tq_kv_read": ([cp, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp], ctypes.c_int),
             "tq_kv_attention_workspace_bytes": ([cp, ctypes.POINTER(TqKvAttn)], ctypes.c_size_t),
             "tq_kv_attention": ([cp, i32, ctypes.POINTER(TqKvAttn), vp], ctypes.c_int),
+            "tq_kv_attention_scope_workspace_bytes": ([cp, ctypes.POINTER(TqKvAttn), ctypes.POINTER(TqKvScope)],
+                                                      ctypes.c_size_t),
+            "tq_kv_attention_scope": ([cp, i32, ctypes.POINTER(TqKvAttn), ctypes.POINTER(TqKvScope), vp], ctypes.c_int),
+            "tq_kv_shared_prefix": ([cp, vp, vp, i32, i32, vp, vp], ctypes.c_int),
+            "tq_rope": ([ctypes.POINTER(TqRopeCall), vp], ctypes.c_int),
+            "tq_logprobs_workspace_bytes": ([ctypes.POINTER(TqLogprobsCall)], ctypes.c_size_t),
+            "tq_logprobs": ([ctypes.POINTER(TqLogprobsCall), vp], ctypes.c_int),
         }
         for name, (args, res) in sigs.items():
             fn = getattr(L, name)
@@ -894,18 +959,51 @@ def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=N
     return k, v
 
 
-def tq_kv_attention_workspace_bytes(cache, n_rows, n_heads, n_tokens=None, max_q=1, max_len=0, window=0):
+def tq_kv_attention_workspace_bytes(cache, n_rows, n_heads, n_tokens=None, max_q=1, max_len=0, window=0, sinks=0,
+                                    n_groups=0, max_prefix=0, max_tail=0):
     """Workspace of tq_kv_attention for n_rows rows of n_tokens queries together
-    (max_q a row without), 0 where it uses none."""
+    (max_q a row without), 0 where it uses none.  n_groups: groups of rows that
+    share a prefix (1 for a call with a prefix and without groups)."""
     T = n_rows * max_q if n_tokens is None else n_tokens
-    _fits(n_rows | T | max_q | n_heads | max_len | window)
+    _fits(n_rows | T | max_q | n_heads | max_len | window | sinks | n_groups | max_prefix | max_tail)
     # (Slots that are not read here: more rows than slots are allowed where rows name theirs.)
     a = TqKvAttn(n_rows, T, max_q, n_heads, max_len, window, 1.0, OUT_FP16, cache.lens.data_ptr())
-    return int(lib().tq_kv_attention_workspace_bytes(cache._ref, a))
+    if not sinks and not n_groups:
+        return int(lib().tq_kv_attention_workspace_bytes(cache._ref, a))
+    some = cache.lens.data_ptr()   # (rows and prefixes are not read here either)
+    return int(lib().tq_kv_attention_scope_workspace_bytes(
+        cache._ref, a, TqKvScope(sinks, n_groups, max_prefix, max_tail, some, some)))
+
+
+def _scope(n, sinks, prefix, groups, max_prefix, max_tail):
+    """tq_kv_scope of n rows, or None where nothing is asked for."""
+    if prefix is None:
+        if groups is not None:
+            raise ValueError("groups share what prefix says")
+        return TqKvScope(sinks, 0, 0, 0, None, None) if sinks else None
+    n_groups = 1 if groups is None else groups.numel() - 1
+    return TqKvScope(sinks, n_groups, max_prefix, max_tail, _i32(groups, n_groups + 1, "groups"),
+                     _i32(prefix, n, "prefix"))
+
+
+def tq_kv_shared_prefix(cache, groups=None, seqs=None, prefix=None, stream=None):
+    """What tq_kv_attention's prefix takes: for every row (slot seqs[i], or slot
+    i) the tokens in the leading pages that all rows of its group name alike,
+    int32 [rows].  Rows groups[g] .. groups[g + 1] - 1 (int32) are a group; all
+    of them without.  Once after the page table changed, for all layers."""
+    n = _n_rows(cache, seqs, None)
+    n_groups = 1 if groups is None else groups.numel() - 1
+    if prefix is None:
+        prefix = torch.empty(n, dtype=torch.int32, device=cache.lens.device)
+    _check(lib().tq_kv_shared_prefix(cache._ref, _i32(seqs, n, "seqs"), _i32(groups, n_groups + 1, "groups"), n_groups, n,
+                                     _i32(prefix, n, "prefix"), _stream(stream)), "tq_kv_shared_prefix")
+    _used_on(stream, seqs, groups, prefix, *cache._buffers())
+    return prefix
 
 
 def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0, scale=None, window=0, o=None,
-                    lse=None, out_f32=False, want_lse=False, workspace=None, stream=None):
+                    lse=None, out_f32=False, want_lse=False, workspace=None, stream=None, sinks=0, prefix=None,
+                    groups=None, max_prefix=0, max_tail=0):
     """Attention of q [T, n_heads, D], the last tokens of their slots, over the
     cache: o [T, n_heads, D] (fp16 or fp32), and with want_lse also the log of
     the softmax's sum, fp32 [T, n_heads].  scale: 1 / sqrt(D) without.  max_q:
@@ -913,13 +1011,22 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
     without it as many as there are tokens, which is right and may be slower
     than a number that fits.  Tokens that no row has are not written.  A
     workspace of the caller's has zeros in its first WORKSPACE_COUNT_BYTES
-    before its first call."""
+    before its first call.
+
+    sinks: the first tokens of a slot that stay visible beside the window.
+    prefix (int32 [rows], from tq_kv_shared_prefix): first tokens that rows of a
+    group have in the same pages; they are attended once for the group.  Rows
+    groups[g] .. groups[g + 1] - 1 are a group, all rows without groups.
+    max_prefix and max_tail say, like max_len, what the caller knows of the
+    longest prefix and the most tokens behind one: they decide how the work is
+    split."""
     T, n_heads, D = q.shape
     n = seqs.numel() if seqs is not None else (cu_q.numel() - 1 if cu_q is not None else T)
     if cu_q is None and n != T:
         raise ValueError("without cu_q, q must have one token a row")
     max_q = _most(max_q, cu_q, T)
-    _fits(layer | max_q | max_len | window)
+    _fits(layer | max_q | max_len | window | sinks | max_prefix | max_tail)
+    scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail) if sinks or prefix is not None or groups is not None else None
     qr = _kv_rows(q, None, cache.head_dim, "q")
     dtype = torch.float32 if out_f32 else torch.float16
     if o is None:
@@ -934,13 +1041,135 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
     a = TqKvAttn(n, T, max_q, n_heads, max_len, window, D ** -0.5 if scale is None else scale,
                  OUT_FP32 if out_f32 else OUT_FP16, _i32(seqs, n, "seqs"), _i32(cu_q, n + 1, "cu_q"), qr,
                  o.data_ptr(), None if lse is None else lse.data_ptr(), None, 0)
-    need = lib().tq_kv_attention_workspace_bytes(cache._ref, a)
+    if scope is None:
+        need = lib().tq_kv_attention_workspace_bytes(cache._ref, a)
+    else:
+        need = lib().tq_kv_attention_scope_workspace_bytes(cache._ref, a, scope)
     if need:
         if workspace is None:
             workspace = cache.attention_workspace(need, stream)
         else:
             _cuda(workspace, torch.uint8, "workspace")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(lib().tq_kv_attention(cache._ref, layer, a, _stream(stream)), "tq_kv_attention")
-    _used_on(stream, q, seqs, cu_q, o, lse, workspace, *cache._buffers())
+    if scope is None:
+        _check(lib().tq_kv_attention(cache._ref, layer, a, _stream(stream)), "tq_kv_attention")
+    else:
+        _check(lib().tq_kv_attention_scope(cache._ref, layer, a, scope, _stream(stream)), "tq_kv_attention_scope")
+    _used_on(stream, q, seqs, cu_q, o, lse, workspace, prefix, groups, *cache._buffers())
     return (o, lse) if lse is not None else o
+
+
+# --------------------------------------------------------------------------
+# Rotary positions and log probabilities.
+# --------------------------------------------------------------------------
+
+def _heads(t, d, name):
+    """fp16 [T, heads, D] on the GPU as tq_kv_rows, any strides but the last."""
+    if not (t.is_cuda and t.dtype == torch.float16 and t.dim() == 3 and t.shape[2] == d and t.stride(2) == 1):
+        raise ValueError(f"{name} must be float16 [tokens, heads, {d}] on the GPU with adjacent channels")
+    return TqKvRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, scale=1.0, q_out=None, k_out=None,
+            stream=None):
+    """Rotary positions of q [T, heads, D] and k [T, kv_heads, D] (None: q
+    alone): channel pair i of the first 2 n channels, n = len(freq), is turned by
+    positions[axis[i], t] * freq[i] radians and scaled.  positions int32 [T], or
+    [axes, T] with axis uint8 [n] (axis 0 without); freq fp32 [n].  The channels
+    of pair i are i and i + n, or 2 i and 2 i + 1 where adjacent.  inverse turns
+    the other way, which is also the gradient.  q_out and k_out: new tensors
+    without; q and k themselves for a call in place.  Returns (q_out, k_out),
+    q_out alone without k."""
+    if q.dim() != 3:
+        raise ValueError("q must be float16 [tokens, heads, D]")
+    T, n_heads, D = q.shape
+    if positions.dim() not in (1, 2) or positions.shape[-1] != T or positions.dtype != torch.int32 or \
+            not positions.is_cuda or (T > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions must be int32 [tokens] or [axes, tokens] on the GPU")
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    _cuda(freq, torch.float32, "freq")
+    if axis is not None:
+        _cuda(axis, torch.uint8, "axis")
+        if axis.numel() != freq.numel():
+            raise ValueError("axis must name one for every frequency")
+    elif axes > 1:
+        raise ValueError("several axes need axis")
+    if k is not None and (k.dim() != 3 or k.shape[0] != T):
+        raise ValueError("k must be float16 [tokens, heads, D]")
+    if q_out is None:
+        q_out = torch.empty((T, n_heads, D), dtype=torch.float16, device=q.device)
+    elif q_out.shape != q.shape:
+        raise ValueError("q_out must have the shape of q")
+    none = TqKvRows(None, 0, 0)
+    kr = ko = none
+    if k is not None:
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=torch.float16, device=q.device)
+        elif k_out.shape != k.shape:
+            raise ValueError("k_out must have the shape of k")
+        kr, ko = _heads(k, D, "k"), _heads(k_out, D, "k_out")
+    call = TqRopeCall(T, n_heads, 0 if k is None else k.shape[1], D, 2 * freq.numel(), axes,
+                      (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0), scale, positions.data_ptr(),
+                      0 if axes == 1 else positions.stride(0), freq.data_ptr(), _ptr(axis), _heads(q, D, "q"), kr,
+                      _heads(q_out, D, "q_out"), ko)
+    _check(lib().tq_rope(call, _stream(stream)), "tq_rope")
+    if stream is not None:
+        _used_on(stream, q, k, positions, freq, axis, q_out, k_out)
+    return q_out if k is None else (q_out, k_out)
+
+
+_logprobs_ws = {}   # by device: workspaces of calls that bring none, one per stream
+
+
+def tq_logprobs_workspace_bytes(n_rows, n_vocab, n_ids=1, n_top=0):
+    """Workspace of tq_logprobs, 0 where it uses none."""
+    _fits(n_rows | n_vocab | n_ids | n_top)
+    return int(lib().tq_logprobs_workspace_bytes(TqLogprobsCall(n_rows, n_vocab, n_ids, n_top, LOGITS_FP16, 1.0, None,
+                                                                n_vocab)))
+
+
+def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=None, workspace=None, stream=None):
+    """Log probabilities under softmax(scale * logits) of rows of logits
+    [T, V] (fp16 or fp32, any row stride): of given tokens ids (int32 [T] or
+    [T, m]), the entropy, and the `top` most likely tokens, the lower index
+    first where logits are equal.  Returns (logp, entropy, top_ids, top_logp):
+    fp32 of the shape of ids, fp32 [T], int32 and fp32 [T, top], None for what
+    was not asked for.  A token outside the vocabulary gets NaN and counts in
+    d_err.  A workspace of the caller's has zeros in its first
+    WORKSPACE_COUNT_BYTES before its first call."""
+    if not (logits.is_cuda and logits.dim() == 2 and logits.dtype in (torch.float16, torch.float32) and
+            (logits.stride(1) == 1 or logits.shape[1] == 1)):
+        raise ValueError("logits must be a float16 or float32 matrix on the GPU with adjacent elements in a row")
+    T, V = logits.shape
+    _fits(T | V | top)
+    f32 = dict(dtype=torch.float32, device=logits.device)
+    logp = entropy = top_ids = top_logp = None
+    m = 0
+    if ids is not None:
+        _cuda(ids, torch.int32, "ids")
+        if ids.dim() not in (1, 2) or ids.shape[0] != T:
+            raise ValueError("ids must be int32 [T] or [T, m]")
+        m = 1 if ids.dim() == 1 else ids.shape[1]
+        logp = torch.empty(ids.shape, **f32)
+    if want_entropy:
+        entropy = torch.empty(T, **f32)
+    if top:
+        top_ids = torch.empty((T, max(top, 0)), dtype=torch.int32, device=logits.device)
+        top_logp = torch.empty((T, max(top, 0)), **f32)
+    call = TqLogprobsCall(T, V, m, top, LOGITS_FP32 if logits.dtype == torch.float32 else LOGITS_FP16, scale,
+                          logits.data_ptr(), logits.stride(0) if T > 1 else V, _ptr(ids), _ptr(logp), _ptr(entropy),
+                          _ptr(top_ids), _ptr(top_logp), _i32(d_err, 1, "d_err"))
+    need = lib().tq_logprobs_workspace_bytes(call)
+    if need:
+        if workspace is None:
+            ws = _logprobs_ws.get(logits.device)
+            if ws is None:
+                ws = _logprobs_ws[logits.device] = _Workspaces(logits.device)
+            workspace = ws.get(need, stream)
+        else:
+            _cuda(workspace, torch.uint8, "workspace")
+        call.workspace, call.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(lib().tq_logprobs(call, _stream(stream)), "tq_logprobs")
+    if stream is not None:
+        _used_on(stream, logits, ids, logp, entropy, top_ids, top_logp, d_err, workspace)
+    return logp, entropy, top_ids, top_logp
