@@ -705,6 +705,7 @@ tq_status tq_rope(const tq_rope_call* call, void* stream);
 #define TQ_LOGITS_FP32 1
 #define TQ_LOGPROBS_MAX_TOP 32
 #define TQ_LOGPROBS_MAX_IDS 1024
+#define TQ_LOGPROBS_MAX_SCALE 1e18f
 
 typedef struct tq_logprobs_call {
   int32_t n_rows;           /* 1 .. 2^20 */
@@ -712,7 +713,7 @@ typedef struct tq_logprobs_call {
   int32_t n_ids;            /* given tokens of a row, 0 .. TQ_LOGPROBS_MAX_IDS */
   int32_t n_top;            /* most likely ones, 0 .. TQ_LOGPROBS_MAX_TOP, at most n_vocab */
   int32_t flags;            /* TQ_LOGITS_FP16 or TQ_LOGITS_FP32 */
-  float scale;              /* finite, > 0 */
+  float scale;              /* > 0, at most TQ_LOGPROBS_MAX_SCALE */
   const void* logits;       /* rows ld >= n_vocab elements apart, aligned to an element */
   int64_t ld;
   const int32_t* ids;       /* device [n_rows][n_ids] */

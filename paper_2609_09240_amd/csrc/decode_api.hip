@@ -29,7 +29,7 @@ tq_status check_logprobs(const tq_logprobs_call* c) {
   if (c->n_rows < 1 || c->n_vocab < 1 || c->n_ids < 0 || c->n_top < 0 || c->n_top > c->n_vocab ||
       c->ld < c->n_vocab)
     return TQ_ERR_SHAPE;
-  if (!isfinite(c->scale) || !(c->scale > 0.0f)) return TQ_ERR_SHAPE;
+  if (!(c->scale > 0.0f) || !(c->scale <= TQ_LOGPROBS_MAX_SCALE)) return TQ_ERR_SHAPE;
   if (c->n_rows > (1 << 20) || c->n_vocab > (1 << 24) || c->n_ids > TQ_LOGPROBS_MAX_IDS ||
       c->n_top > TQ_LOGPROBS_MAX_TOP || (c->flags != TQ_LOGITS_FP16 && c->flags != TQ_LOGITS_FP32))
     return TQ_ERR_UNSUPPORTED;

@@ -26,7 +26,8 @@ hipError_t launch_kv_attention(const KvDev& c, int layer, const AttnCall& call, 
   if (!plan(c, call, &p)) return hipErrorInvalidValue;
   Args a;
   fill(a, c, layer, call, p);
-  return start<kPlain>(c, a, p, s);
+  const dim3 grid = p.shares ? dim3(p.shares) : dim3(a.H, a.n_rows, p.tiles);
+  return with_sizes(c, [&](auto D, auto G) { kv_attn_kernel<D(), G(), kPlain><<<grid, 64 * kWaves, 0, s>>>(a); });
 }
 
 }  // namespace tq

@@ -47,6 +47,8 @@
 
 #pragma once
 
+#include <type_traits>
+
 #include "q4_internal.h"
 
 namespace tq {
@@ -65,6 +67,7 @@ constexpr int kCus = 256;
 constexpr int kMinUnits = 4;
 constexpr int kUnitsOfShare = 2;
 constexpr int kMaxShares = 4 * kCus;
+constexpr int kMaxParts = 32;   // of a row's own tokens, and of shared ones, where the host decides
 constexpr int kOneLevel = 16;   // parts joined in one step (96 of them: 47 us in one step, 40 in two)
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -132,11 +135,13 @@ __device__ inline float over_power(float x) {
 }
 __device__ inline float log2_of(float x) { return (float)((int)(__builtin_bit_cast(uint32_t, x) >> 23) - 127); }
 
-// What a launch does.  kPlain: rows over their own tokens.  kSinks: the first
-// tokens of a slot beside a window.  kStack: a group of rows over the tokens
-// that they share, their queries stacked as the rows of one tile after the other;
-// leaves sums.  kRest: rows over what is behind the shared tokens; takes those sums up.
-enum { kPlain, kSinks, kStack, kRest };
+// What a launch does.  kPlain: rows over their own tokens, the work divided on
+// the device.  The others take tiles in parts that the host decides, and where
+// there are several leave sums that kv_join_kernel joins.  kSinks: the first tokens
+// of a slot beside a window.  kShared: groups of rows over the tokens that they share
+// (stacked: the queries of all of a group's rows as the rows of its tiles), and
+// rows over what is behind those.
+enum { kPlain, kSinks, kShared };
 
 struct Args {
   const uint8_t* layer;    // the layer's pages
@@ -161,12 +166,14 @@ struct Args {
 };
 
 struct MoreArgs : Args {
-  const int32_t* cu_rows;  // kStack: rows of the groups, NULL: one group of all
+  const int32_t* cu_rows;  // rows of the groups, NULL: one group of all
   const int32_t* prefix;   // [rows] shared tokens of a row
-  float* pre;              // what shared tokens give: [parts][n_tokens * heads][D + 4], sums, reference (log2), sum of p
+  float* pre;              // [parts][n_tokens * heads][D + 4]: sums, reference (log2), sum of p
   int64_t pre_part;        // floats of a part
-  int32_t pre_parts;
-  int32_t all_rows;        // kStack: rows of the call (n_rows: its groups)
+  int32_t parts;           // of a row's own tokens
+  int32_t stack_parts;     // of shared tokens; those parts come first
+  int32_t stack_blocks;    // workgroups of kv_attn_kernel for those, before the others
+  int32_t stack_tiles, n_groups;
   int32_t sinks;
 };
 
@@ -179,8 +186,8 @@ struct ArgsFor<kPlain> {
   typedef Args type;
 };
 
-// What a tile of rows is: row b of the call (kStack: its group b), key/value
-// head h, tile qt.
+// What a tile of rows is: row b of the call (stacked: the group that starts
+// there), key/value head h, tile qt.
 struct Tile {
   int b, h, qt;
   int seq, first, n, rows;   // slot, first token in q, tokens, rows of (b, h) in all
@@ -190,8 +197,8 @@ struct Tile {
   int rec0, rec1;            // records it can see
   int units;                 // of four records, one a wave; 1 where there are none
   int win0;                  // kSinks: records rec0 .. win0 - 1 stand for the first ones of the slot
-  int b1;                    // kStack: the group's rows are b .. b1 - 1
-  int shared;                // kRest: tokens whose sums are there
+  int b1;                    // stacked: the group's rows are b .. b1 - 1
+  int shared;                // kShared: tokens whose sums the group's tiles give
 };
 
 // x / share for x < share + 16 <= 2^16.
@@ -213,11 +220,12 @@ __device__ inline int shared_of(const MoreArgs& a, int row) {
   return (int)min(max((int64_t)as_table(a.prefix)[row], (int64_t)0), most) & ~31;
 }
 
-// Tile qt of group g, whose pages are those of its first row that shares any;
-// false where there is none.
+// Tile qt (of R rows) of group g, whose pages are those of its first row that
+// shares any; false where there is none.
+template <int R>
 __device__ inline bool stack_of(const MoreArgs& a, int g, int qt, Tile* t) {
-  const int r0 = a.cu_rows ? as_table(a.cu_rows)[g] : 0, r1 = a.cu_rows ? as_table(a.cu_rows)[g + 1] : a.all_rows;
-  if (r0 < 0 || r1 > a.all_rows) return false;
+  const int r0 = a.cu_rows ? as_table(a.cu_rows)[g] : 0, r1 = a.cu_rows ? as_table(a.cu_rows)[g + 1] : a.n_rows;
+  if (r0 < 0 || r1 > a.n_rows) return false;
   int lead = r0;
   while (lead < r1 && as_table(a.prefix)[lead] < 32) ++lead;
   if (lead >= r1) return false;
@@ -231,7 +239,7 @@ __device__ inline bool stack_of(const MoreArgs& a, int g, int qt, Tile* t) {
   t->n = first < 0 || end <= first ? 0 : end - first;
   t->asked = t->n;
   t->rows = t->n * a.share;
-  t->row0 = qt * 16;
+  t->row0 = qt * R;
   if (t->row0 >= t->rows) return false;
   t->tok0 = qt == 0 ? 0 : t->row0 / a.share;
   t->head0 = t->row0 - t->tok0 * a.share;
@@ -266,10 +274,9 @@ __device__ inline int stack_pos(const MoreArgs& a, int b, int b1, int at) {
   return (int)max(min((int64_t)shared, len - asked + i + 1), (int64_t)0) - 1;
 }
 
-// Tile (b, qt) of head 0; false where there is none.
-template <int MODE, class A>
+// Tile (b, qt) of R rows of head 0; false where there is none.
+template <int MODE, int R = 16, class A>
 __device__ inline bool tile_of(const A& a, int b, int qt, Tile* t) {
-  if constexpr (MODE == kStack) return stack_of(a, b, qt, t);
   t->h = 0;
   t->b = b;
   t->qt = qt;
@@ -281,17 +288,17 @@ __device__ inline bool tile_of(const A& a, int b, int qt, Tile* t) {
   t->first = (int)first;
   t->n = bad || end <= first ? 0 : (int)(end - first);
   t->rows = t->n * a.share;
-  t->row0 = qt * 16;
+  t->row0 = qt * R;
   if (t->row0 >= t->rows) return false;
   t->tok0 = qt == 0 ? 0 : t->row0 / a.share;
   t->head0 = t->row0 - t->tok0 * a.share;
   t->len = length_of(a, t->seq);
   // Position of query token i is base + i; all of what was asked for counts.
   const int64_t base = t->len - asked;
-  const int last = min(t->tok0 + by_share(a, t->head0 + 15), t->n - 1);
+  const int last = min(t->tok0 + by_share(a, t->head0 + R - 1), t->n - 1);
   const int64_t hi = min((int64_t)t->len, base + last + 1);
   int64_t lo = a.window > 0 ? max((int64_t)0, base + t->tok0 + 1 - a.window) : 0;
-  if constexpr (MODE == kRest) lo = t->shared = shared_of(a, b);
+  if constexpr (MODE == kShared) lo = t->shared = shared_of(a, b);
   t->rec0 = (int)(lo >> 5);
   t->rec1 = hi > lo ? (int)((hi + 31) >> 5) : t->rec0;
   if constexpr (MODE == kSinks) {
@@ -302,32 +309,17 @@ __device__ inline bool tile_of(const A& a, int b, int qt, Tile* t) {
   return true;
 }
 
-// o and lse of row r of a tile: four channels of the joined sum y, what it is
-// divided by, the reference.
-template <int MODE, class A>
-__device__ inline void store_row(const A& a, const Tile& t, int D, int r, int d, float4v y, float sum, float ref) {
+// Where row r of a tile stands among all queries and heads.
+template <class A>
+__device__ inline int64_t place_of(const A& a, const Tile& t, int r) {
   const int tok = by_share(a, t.head0 + r), head = t.head0 + r - tok * a.share;
-  const int64_t at = (int64_t)(t.first + t.tok0 + tok) * (a.H * a.share) + t.h * a.share + head;
-  if constexpr (MODE == kStack) {
-    float* p = a.pre + at * (D + 4);
-    *reinterpret_cast<float4v*>(p + d) = y;
-    if (d == 0) *reinterpret_cast<float4v*>(p + D) = float4v{ref, sum, 0, 0};
-    return;
-  }
-  if constexpr (MODE == kRest) {
-    // The parts of the shared tokens, in their order.
-    for (int k = 0; t.shared > 0 && k < a.pre_parts; ++k) {
-      const float* p = a.pre + k * a.pre_part + at * (D + 4);
-      const float4v v = *reinterpret_cast<const float4v*>(p + d), x = *reinterpret_cast<const float4v*>(p + D);
-      const float top = fmaxf(ref, x[0]);
-      const float f = ref == -__builtin_inff() ? 0.0f : exp2f(ref - top);
-      const float g = x[0] == -__builtin_inff() ? 0.0f : exp2f(x[0] - top);
-      sum = fmaf(x[1], g, sum * f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], g, y[i] * f);
-      ref = top;
-    }
-  }
+  return (int64_t)(t.first + t.tok0 + tok) * (a.H * a.share) + t.h * a.share + head;
+}
+
+// o and lse of a query and head: four channels of the joined sum y, what it is
+// divided by, the reference.
+template <class A>
+__device__ inline void store_at(const A& a, int64_t at, int D, int d, float4v y, float sum, float ref) {
   y *= sum == 0.0f ? 0.0f : 1.0f / sum;
   if (a.out_f32) {
     *reinterpret_cast<float4v*>(static_cast<float*>(a.o) + at * D + d) = y;
@@ -336,6 +328,19 @@ __device__ inline void store_row(const A& a, const Tile& t, int D, int r, int d,
     *reinterpret_cast<half4*>(static_cast<uint16_t*>(a.o) + at * D + d) = z;
   }
   if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -__builtin_inff() : (ref + log2f(sum)) * kLn2;
+}
+
+template <class A>
+__device__ inline void store_row(const A& a, const Tile& t, int D, int r, int d, float4v y, float sum, float ref) {
+  store_at(a, place_of(a, t, r), D, d, y, sum, ref);
+}
+
+// The sums of a part instead.
+__device__ inline void store_part(const MoreArgs& a, const Tile& t, int D, int r, int d, float4v y, float sum, float ref,
+                                  int part) {
+  float* p = a.pre + part * a.pre_part + place_of(a, t, r) * (D + 4);
+  *reinterpret_cast<float4v*>(p + d) = y;
+  if (d == 0) *reinterpret_cast<float4v*>(p + D) = float4v{ref, sum, 0, 0};
 }
 
 // Even shares: the units of all tiles and heads in a line (tiles by qt, then
@@ -355,8 +360,7 @@ __device__ inline int share_with(const Share& s, int unit) {
   const int head = s.more * (s.q + 1);
   return unit < head ? unit / (s.q + 1) : s.more + (unit - head) / s.q;
 }
-template <int MODE, class A>
-__device__ inline Share share_of(const A& a) {
+__device__ inline Share share_of(const Args& a) {
   const int lane = threadIdx.x & 63, pairs = a.n_rows * a.tiles, per = (pairs + 63) >> 6;
   int n[kMaxPairs / 64], sum = 0;
 #pragma unroll
@@ -366,7 +370,7 @@ __device__ inline Share share_of(const A& a) {
     if (e < per && i < pairs) {
       Tile t;
       const int qt = a.tiles == 1 ? 0 : i / a.n_rows;
-      if (tile_of<MODE>(a, i - qt * a.n_rows, qt, &t)) n[e] = t.units * a.H;
+      if (tile_of<kPlain>(a, i - qt * a.n_rows, qt, &t)) n[e] = t.units * a.H;
     }
     sum += n[e];
   }
@@ -419,19 +423,20 @@ __device__ inline A args_anew() {
 // that cost moves).
 constexpr int waves_of(int D, int G) { return D == 64 ? 4 : D == 128 ? (G == 32 ? 2 : 3) : 1; }
 
-template <int D, int G, int MODE>
-__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(waves_of(D, G))))
+template <int D, int G, int MODE, int W = kWaves>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(waves_of(D, G))))
 kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   typedef typename ArgsFor<MODE>::type A;
   constexpr int NG = D / G, J = G / 32, KD = D / 32, VD = D / 16;
   constexpr int64_t kRec = 32 * (D + 8 * NG);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane >> 4;
-  __shared__ float sm[kWaves][16], sl[kWaves][16];
-  __shared__ float so[kWaves][16][D + 4];
+  __shared__ float sm[W][16], sl[W][16];
+  __shared__ float so[W][16][D + 4];
   __shared__ int arrived;
   Share share = {1, 0, 0, 1, 0, 0};
-  if (args.shares > 0) share = share_of<MODE>(args);
+  if constexpr (MODE == kPlain)
+    if (args.shares > 0) share = share_of(args);
   const int first_unit = share.unit;
   Tile t;
   int h = 0;
@@ -439,10 +444,26 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   // The tiles, or parts of tiles, of the workgroup: one, or those of its share.
   while (share.unit < share.end) {
   const A a = args_anew<A>();
-  int rec0, rec1, head_unit = 0;
-  bool all_of_it = true;
+  int rec0, rec1, head_unit = 0, part = 0;
+  bool all_of_it = true, stacked = false;
   const int slot = 2 * blockIdx.x + (share.unit != first_unit);
-  if (a.shares > 0) {
+  if constexpr (MODE != kPlain) {
+    // Heads beside each other, then parts, rows, tiles.
+    int id = blockIdx.x;
+    stacked = MODE == kShared && id < a.stack_blocks;
+    if (MODE == kShared && !stacked) id -= a.stack_blocks;
+    const int parts = stacked ? a.stack_parts : a.parts, n = stacked ? a.n_groups : a.n_rows;
+    const int i = id / a.H, j = i / parts, qt = j / n;
+    part = i - j * parts;
+    if (!(stacked ? stack_of<16>(a, j - qt * n, qt, &t) : tile_of<MODE>(a, j - qt * n, qt, &t))) return;
+    t.h = id - i * a.H;
+    const int64_t all = t.rec1 - t.rec0;
+    rec0 = t.rec0 + (int)(all * part / parts);
+    rec1 = t.rec0 + (int)(all * (part + 1) / parts);
+    all_of_it = MODE == kSinks && parts == 1;
+    if (MODE == kShared && !stacked) part += a.stack_parts;
+    share.unit = share.end;
+  } else if (a.shares > 0) {
     if (fresh) {
       for (;; ++share.pair) {   // there is one: units are left
         const int qt = a.tiles == 1 ? 0 : share.pair / a.n_rows;
@@ -493,7 +514,7 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   const int per_shift = a.page_shift - 5;
   const table_ptr row_pages = as_table(a.pages) + (int64_t)(t.len > 0 ? t.seq : 0) * a.max_pages;
   auto next_record = [&](int* rec) -> const uint8_t* {
-    for (; *rec < rec1; *rec += kWaves) {
+    for (; *rec < rec1; *rec += W) {
       const int at = in_slot(*rec), page = row_pages[at >> per_shift];
       if (page >= 0 && page < a.n_pages) {
         const int per = 1 << per_shift;
@@ -562,10 +583,9 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   const uint16_t* qp = a.q + (int64_t)(t.first + tok) * a.q_ts + head * a.q_hs;
   pos = -1;
   if (in) {
-    if constexpr (MODE == kStack)
-      pos = stack_pos(a, t.b, t.b1, t.first + tok);
-    else
-      pos = (int)max(base + tok, (int64_t)-1);
+    pos = (int)max(base + tok, (int64_t)-1);
+    if constexpr (MODE == kShared)
+      if (stacked) pos = stack_pos(a, t.b, t.b1, t.first + tok);
   }
 #pragma unroll
   for (int j = 0; j < KD; ++j) q[j] = in ? load8(qp + 32 * j + 8 * qc) : zero;
@@ -588,11 +608,12 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
     const int last = min(t.tok0 + by_share(a, t.head0 + 15), t.n - 1);
     all1 = (int)max((int64_t)0, min((int64_t)t.len, base + t.tok0 + 1));
     if (a.window > 0) all0 = (int)max((int64_t)0, base + last + 1 - a.window);
-    if constexpr (MODE == kStack) {
-      all1 = in ? pos + 1 : INT32_MAX;
+    if constexpr (MODE == kShared)
+      if (stacked) {   // tokens that the call leaves out see nothing; nobody takes up what they get
+        all1 = in && pos >= 0 ? pos + 1 : INT32_MAX;
 #pragma unroll
-      for (int k = 1; k < 16; k *= 2) all1 = min(all1, __shfl_xor(all1, k));
-    }
+        for (int k = 1; k < 16; k *= 2) all1 = min(all1, __shfl_xor(all1, k));
+      }
     all0 = uniform(all0);
     all1 = uniform(all1);
   }
@@ -632,7 +653,7 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   while (at != nullptr) {
     // A register's record is replaced by the next one's as soon as it is used,
     // so that a load has nearly a whole pass to arrive in.
-    int rec_n = rec + kWaves;
+    int rec_n = rec + W;
     const uint8_t* at_n = next_record(&rec_n);
     const uint8_t* pf = at_n != nullptr ? at_n : at;
     const int t0 = 32 * in_slot(rec);   // the record's first token
@@ -790,8 +811,6 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   int tx = threadIdx.x;
   asm volatile("" : "+v"(tx));
   const A z = args_anew<A>();
-  const __amdgpu_buffer_rsrc_t parts_of =
-      __builtin_amdgcn_make_buffer_rsrc(z.part, 0, 2 * z.shares * z.R * (D + 4) * 4, 0x00020000);
   const int oc = (tx >> 4) & 3, ocol = tx & 15;
   const float m = grow == kNone ? -__builtin_inff() : ref;
   float L = l;
@@ -808,7 +827,7 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   __syncthreads();
   float top = sm[0][ocol];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm[w][ocol]);
+  for (int w = 1; w < W; ++w) top = fmaxf(top, sm[w][ocol]);
   const float f = m == -__builtin_inff() ? 0.0f : exp2f(m - top);
   if (oc == 0) sl[wave][ocol] = L * f;
 #pragma unroll
@@ -820,25 +839,30 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
     if (t.row0 + ocol < t.rows) *reinterpret_cast<float4v*>(&so[wave][ocol][16 * j + 4 * oc]) = y;
   }
   __syncthreads();
-  for (int i = tx; i < 16 * D / 4; i += 64 * kWaves) {
+  const __amdgpu_buffer_rsrc_t parts_of =
+      __builtin_amdgcn_make_buffer_rsrc(z.part, 0, 2 * z.shares * z.R * (D + 4) * 4, 0x00020000);
+  for (int i = tx; i < 16 * D / 4; i += 64 * W) {
     const int r = i / (D / 4), d = i % (D / 4) * 4, row = t.row0 + r;
     if (row >= t.rows) continue;
     float4v y = *reinterpret_cast<float4v*>(&so[0][r][d]);
     float sum = sl[0][r], most = sm[0][r];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
+    for (int w = 1; w < W; ++w) {
       y += *reinterpret_cast<float4v*>(&so[w][r][d]);
       sum += sl[w][r];
       most = fmaxf(most, sm[w][r]);
     }
     if (all_of_it) {
-      store_row<MODE>(z, t, D, r, d, y, sum, most);
+      store_row(z, t, D, r, d, y, sum, most);
+    } else if constexpr (MODE != kPlain) {
+      store_part(z, t, D, r, d, y, sum, most, part);
     } else {
       const int p = (slot * z.R + r) * (D + 4) * 4;
       put4(parts_of, p + 4 * d, y);
       if (d == 0) put4(parts_of, p + 4 * D, float4v{most, sum, 0, 0});
     }
   }
+  if constexpr (MODE != kPlain) return;
   if (all_of_it) continue;
 
   // The last workgroup of a tile to leave its part joins them all, in the
@@ -928,7 +952,7 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
         for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], g, y[i]);
       }
       if (last) {
-        store_row<MODE>(z, t, D, r, d, y, sum, top);
+        store_row(z, t, D, r, d, y, sum, top);
       } else {
         const int p = (slot_of(first) * z.R + r) * (D + 4) * 4;
         put4(parts_of, p + 4 * d, y);
@@ -943,6 +967,70 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   first = 0;
   }
   }
+}
+
+// o and lse of one query and head from the sums of their parts, in the order of
+// the parts; a row that shares nothing has its own parts only.  D/4 threads of
+// every group of them take four channels each, the groups the parts in turn, all
+// of them on their way at once: a trip to memory for the row, one for the sums,
+// and lengths do not matter (a part that saw nothing says so).
+template <int D, int MODE>
+__global__ void __launch_bounds__(256) kv_join_kernel(MoreArgs a) {
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAhead = 2 * kMaxParts / kGroups;
+  __shared__ float4v ys[kGroups][kLanes];
+  __shared__ float refs[kGroups], sums[kGroups];
+  const int b = blockIdx.y, heads = a.H * a.share;
+  const int64_t first = a.cu ? as_table(a.cu)[b] : b, end = a.cu ? as_table(a.cu)[b + 1] : (int64_t)b + 1;
+  const int k1 = a.stack_parts + a.parts;
+  const int k0 = MODE == kShared && shared_of(a, b) == 0 ? a.stack_parts : 0;
+  const int64_t at = (first + blockIdx.z) * heads + blockIdx.x;
+  if (first < 0 || first + blockIdx.z >= min(end, (int64_t)a.n_tokens)) return;
+  const int grp = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
+  const float* p = a.pre + at * (D + 4);
+  float4v v[kAhead], x[kAhead];
+#pragma unroll
+  for (int e = 0; e < kAhead; ++e) {
+    const int k = k0 + grp + e * kGroups;
+    x[e] = float4v{-__builtin_inff(), 0, 0, 0};
+    v[e] = float4v{0, 0, 0, 0};
+    if (k < k1) {
+      v[e] = *reinterpret_cast<const float4v*>(p + k * a.pre_part + 4 * l);
+      x[e] = *reinterpret_cast<const float4v*>(p + k * a.pre_part + D);
+    }
+  }
+  float ref = x[0][0], sum = 0.0f;
+#pragma unroll
+  for (int e = 1; e < kAhead; ++e) ref = fmaxf(ref, x[e][0]);
+  float4v y = {0, 0, 0, 0};
+  auto weight = [](float m, float top) { return m == -__builtin_inff() ? 0.0f : exp2f(m - top); };
+#pragma unroll
+  for (int e = 0; e < kAhead; ++e) {
+    const float g = weight(x[e][0], ref);
+    sum = fmaf(x[e][1], g, sum);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = fmaf(v[e][j], g, y[j]);
+  }
+  ys[grp][l] = y;
+  if (l == 0) {
+    refs[grp] = ref;
+    sums[grp] = sum;
+  }
+  __syncthreads();
+  if (grp != 0) return;
+  float top = refs[0];
+#pragma unroll
+  for (int i = 1; i < kGroups; ++i) top = fmaxf(top, refs[i]);
+  sum = 0.0f;
+  y = float4v{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    const float g = weight(refs[i], top);
+    const float4v w = ys[i][l];
+    sum = fmaf(sums[i], g, sum);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = fmaf(w[j], g, y[j]);
+  }
+  store_at(a, at, D, 4 * l, y, sum, top);
 }
 
 // The split of a launch: `rows` rows of queries and heads at most in each of
@@ -1014,24 +1102,20 @@ inline void fill(Args& a, const KvDev& c, int layer, const AttnCall& call, const
   a.out_f32 = call.out_f32;
 }
 
-template <int D, int G, int MODE, class A>
-void start(const A& a, const Plan& p, hipStream_t s) {
-  const dim3 grid = p.shares ? dim3(p.shares) : dim3(a.H, a.n_rows, p.tiles);
-  kv_attn_kernel<D, G, MODE><<<grid, 64 * kWaves, 0, s>>>(a);
-}
-
-template <int MODE, class A>
-hipError_t start(const KvDev& c, const A& a, const Plan& p, hipStream_t s) {
+// f(D, G) of a cache, as constants.
+template <class F>
+hipError_t with_sizes(const KvDev& c, F f) {
+  using std::integral_constant;
+  integral_constant<int, 32> a;
+  integral_constant<int, 64> b;
+  integral_constant<int, 128> d;
+  integral_constant<int, 256> e;
   if (c.D == 64) {
-    c.G == 32 ? start<64, 32, MODE>(a, p, s) : start<64, 64, MODE>(a, p, s);
+    c.G == 32 ? f(b, a) : f(b, b);
   } else if (c.D == 128) {
-    c.G == 32   ? start<128, 32, MODE>(a, p, s)
-    : c.G == 64 ? start<128, 64, MODE>(a, p, s)
-                : start<128, 128, MODE>(a, p, s);
+    c.G == 32 ? f(d, a) : c.G == 64 ? f(d, b) : f(d, d);
   } else {
-    c.G == 32   ? start<256, 32, MODE>(a, p, s)
-    : c.G == 64 ? start<256, 64, MODE>(a, p, s)
-                : start<256, 128, MODE>(a, p, s);
+    c.G == 32 ? f(e, a) : c.G == 64 ? f(e, b) : f(e, d);
   }
   return hipGetLastError();
 }

@@ -4,48 +4,135 @@
 // Sinks: the records of a tile are those of its window and, in front of them,
 // the first ones of the slot; masks in the records where they end.
 //
-// Shared prefixes, two launches.  The softmax over all tokens of a row is joined
-// from those over any parts of them: with m the largest logit of a part, l = sum
-// exp(s - m) and y = sum exp(s - m) v,
+// Shared prefixes.  The softmax over all tokens of a row is joined from those over
+// any parts of them: with m the largest logit of a part, l = sum exp(s - m) and
+// y = sum exp(s - m) v,
 //     o = sum_parts exp(m - M) y / sum_parts exp(m - M) l,   M = max of the m.
-// The first launch takes the queries of all rows of a group as the rows of its
-// tiles, over the shared records, and leaves (y, m, l) of every query and head.
-// The second one is a row over its own records, which takes them up when it
-// stores.
+// One launch takes the queries of all rows of a group as the rows of its tiles
+// over the shared records, and every row over what it has behind them; a second
+// one joins.
 
 #include "decode_internal.h"
 #include "kvattn_kernel.h"
+#include "kvwide.h"
 
 namespace tq {
 namespace {
 
 struct ScopePlan {
   bool plain, sinks;    // neither: shared
-  Plan all, stack, rest;
-  size_t parts, pre;    // bytes behind the counts
+  int waves;            // of a workgroup of kv_attn_kernel
+  int tiles, parts;     // of a row, 16 query rows each; of its own tokens
+  int stack_tiles, stack_parts;   // of a group
+  int wide;             // kv_wide_kernel for the stacked (or all) rows, with so many tiles of 16 rows a wave; 0: not
+  size_t bytes;         // workspace behind the counts
 };
+
+// Parts of `recs` records of each of `ids` tiles and heads, and what they take (us):
+// a wave needs 1 us for a record where it is alone on its SIMD, and 0.6 where others
+// work there; joining parts takes `join`.
+double split(int64_t ids, int64_t recs, int waves, double join, int* parts) {
+  double best = 1e30;
+  for (int n = 1; n <= kMaxParts; n += n < 4 ? 1 : n / 4) {
+    if (n > 1 && recs < 2 * (int64_t)waves * n) break;
+    const double load = (double)ids * n * waves / (4 * kCus), each = 0.6 * load > 1.0 ? 0.6 * load : 1.0;
+    const double t = (double)((recs + (int64_t)n * waves - 1) / ((int64_t)n * waves)) * each + (n > 1 ? join : 0.0);
+    if (t < 0.95 * best) {
+      best = t;
+      *parts = n;
+    }
+  }
+  return best;
+}
 
 bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) {
   const int share = a.n_heads / c.H;
+  const int64_t rows = (int64_t)a.max_q * share, tiles = (rows + 15) / 16, ids = tiles * a.n_rows * c.H;
+  const int64_t hint = length_hint(c, a), part_bytes = (int64_t)a.n_tokens * a.n_heads * (c.D + 4) * 4;
+  // What a grid holds: with 256 threads a workgroup, and with 512 of two kinds.
+  constexpr int64_t kMostIds = 1 << 23, kMostOfTwo = 1 << 21;
   p->plain = p->sinks = false;
-  if (sc.n_groups > 0 && a.window == 0) {
-    const int64_t prefix = sc.max_prefix > 0 ? sc.max_prefix : length_hint(c, a);
-    const int64_t tail = sc.max_tail > 0 ? (int64_t)sc.max_tail + 31 : length_hint(c, a);
-    if (plan(c, (int64_t)a.n_tokens * share, sc.n_groups, prefix, &p->stack) &&
-        plan(c, (int64_t)a.max_q * share, a.n_rows, tail, &p->rest)) {
-      const size_t x = part_bytes(c, p->stack), y = part_bytes(c, p->rest);
-      p->parts = x > y ? x : y;
-      p->pre = (size_t)a.n_tokens * a.n_heads * (c.D + 4) * 4;
-      return true;
+  p->wide = p->stack_parts = p->stack_tiles = 0;
+  p->waves = c.D == 256 ? 4 : 8;
+  p->tiles = (int)tiles;
+  p->bytes = 0;
+  if (tiles > 65535 || ids > kMostIds) return false;
+  const bool joined = a.max_q <= 65535;   // a grid of rows and tokens
+  if (sc.n_groups > 0 && a.window == 0 && joined) {
+    const int64_t stacked = (int64_t)a.n_tokens * share, of_group = stacked / sc.n_groups;
+    const int64_t prefix = (sc.max_prefix > 0 ? sc.max_prefix : hint) / 32;
+    const int64_t tail = (sc.max_tail > 0 ? (int64_t)sc.max_tail + 31 : hint) / 32 + 1;
+    const int64_t stack_tiles = (stacked + 15) / 16, stack_ids = (stack_tiles + sc.n_groups) * c.H;
+    if (stack_tiles <= 65535 && ids <= kMostOfTwo && stack_tiles * sc.n_groups * c.H <= kMostOfTwo) {
+      p->stack_tiles = (int)stack_tiles;
+      const double t = split(stack_ids, prefix, p->waves, 0.0, &p->stack_parts) +
+                       0.5 * split(ids, tail, p->waves, 0.0, &p->parts) + 6.0;
+      int n;
+      const double alone = split(ids, prefix + tail, 4, 8.0, &n);
+      if (t < alone) {
+        if (of_group >= 48 && share <= 1024 && stack_ids * prefix > 60000) {
+          p->wide = 1;
+          const int64_t n = (stacked + 63) / 64 + sc.n_groups;
+          p->stack_tiles = (int)((stacked + 63) / 64);
+          int64_t q = (3 * kCus + n * c.H - 1) / (n * c.H);
+          q = q < prefix / 8 ? q : prefix / 8;
+          p->stack_parts = (int)(q < 1 ? 1 : q < kMaxParts ? q : kMaxParts);
+        }
+        p->bytes = (size_t)(p->parts + p->stack_parts) * part_bytes;
+        return true;
+      }
     }
   }
+  p->stack_parts = 0;
   p->sinks = a.window > 0 && sc.sinks > 0;
   p->plain = !p->sinks;
   if (p->plain) return true;
-  int64_t len = length_hint(c, a);
-  const int64_t most = (int64_t)a.window + a.max_q + sc.sinks + 31;
-  if (len > most) len = most;
-  return plan(c, (int64_t)a.max_q * share, a.n_rows, len, &p->all);
+  const int64_t most = (int64_t)a.window + a.max_q + sc.sinks + 31, len = hint < most ? hint : most;
+  int parts4;
+  const double t4 = split(ids, len / 32 + 1, 4, 6.0, &parts4);
+  const double t8 = split(ids, len / 32 + 1, 8, 6.0, &p->parts);
+  if (p->waves == 4 || t4 <= t8 || ids > kMostOfTwo || !joined) {
+    p->waves = 4;
+    p->parts = parts4;
+  }
+  if (!joined) p->parts = 1;
+  if (p->parts > 1) p->bytes = (size_t)p->parts * part_bytes;
+  return true;
+}
+
+template <int MODE>
+hipError_t start(const KvDev& c, const MoreArgs& a, const ScopePlan& p, hipStream_t s) {
+  const dim3 grid(a.stack_blocks + a.H * a.parts * a.n_rows * a.tiles);
+  return with_sizes(c, [&](auto D, auto G) {
+    if constexpr (D() != 256)
+      if (p.waves == 8) {
+        kv_attn_kernel<D(), G(), MODE, 8><<<grid, 64 * 8, 0, s>>>(a);
+        return;
+      }
+    if constexpr (D() == 256 || MODE == kSinks) kv_attn_kernel<D(), G(), MODE, 4><<<grid, 64 * 4, 0, s>>>(a);
+  });
+}
+
+template <int MODE>
+hipError_t start_wide(const KvDev& c, const MoreArgs& a, const ScopePlan& p, hipStream_t s) {
+  return with_sizes(c, [&](auto D, auto G) {
+    if constexpr (MODE == kShared) {
+      const dim3 grid(a.H * a.stack_parts, a.n_groups, p.stack_tiles);
+      kv_wide_kernel<D(), G(), MODE, 1><<<grid, 256, 0, s>>>(a);
+    }
+  });
+}
+
+template <int MODE>
+hipError_t start_join(const KvDev& c, const MoreArgs& a, hipStream_t s) {
+  const dim3 grid(a.H * a.share, a.n_rows, a.max_q);
+  if (c.D == 64)
+    kv_join_kernel<64, MODE><<<grid, 256, 0, s>>>(a);
+  else if (c.D == 128)
+    kv_join_kernel<128, MODE><<<grid, 256, 0, s>>>(a);
+  else
+    kv_join_kernel<256, MODE><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 // The leading pages that the rows of a group name alike.  A workgroup takes a
@@ -107,10 +194,7 @@ bool kv_scope_plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, size_
   ScopePlan p;
   if (!plan(c, a, sc, &p)) return false;
   if (p.plain) return kv_attention_plan(c, a, ws_bytes);
-  if (p.sinks)
-    *ws_bytes = p.all.shares > 0 ? kCountBytes + part_bytes(c, p.all) : 0;
-  else
-    *ws_bytes = kCountBytes + p.parts + p.pre;
+  *ws_bytes = p.bytes > 0 ? kCountBytes + p.bytes : 0;
   return true;
 }
 
@@ -120,26 +204,29 @@ hipError_t launch_kv_attention_scope(const KvDev& c, int layer, const AttnCall& 
   if (!plan(c, call, sc, &p)) return hipErrorInvalidValue;
   if (p.plain) return launch_kv_attention(c, layer, call, s);
   MoreArgs a;
+  fill(a, c, layer, call, Plan{p.tiles, 0, 0, 0});
   a.cu_rows = sc.cu_rows;
   a.prefix = sc.prefix;
-  a.pre = nullptr;
-  a.pre_part = 0;
-  a.pre_parts = 0;
-  a.all_rows = call.n_rows;
-  a.sinks = sc.sinks;
-  if (p.sinks) {
-    fill(a, c, layer, call, p.all);
-    return start<kSinks>(c, a, p.all, s);
-  }
-  a.pre = reinterpret_cast<float*>(static_cast<uint8_t*>(call.ws) + kCountBytes + p.parts);
+  a.pre = a.part;   // behind the counts, which are not used
   a.pre_part = (int64_t)call.n_tokens * call.n_heads * (c.D + 4);
-  a.pre_parts = 1;
-  fill(a, c, layer, call, p.stack);
-  a.n_rows = sc.n_groups;
-  hipError_t e = start<kStack>(c, a, p.stack, s);
-  if (e != hipSuccess) return e;
-  fill(a, c, layer, call, p.rest);
-  return start<kRest>(c, a, p.rest, s);
+  a.parts = p.parts;
+  a.stack_parts = p.stack_parts;
+  a.stack_tiles = p.stack_tiles;
+  a.n_groups = sc.n_groups;
+  a.stack_blocks = 0;
+  a.sinks = sc.sinks;
+  hipError_t e;
+  if (p.sinks) {
+    e = start<kSinks>(c, a, p, s);
+    return e == hipSuccess && p.parts > 1 ? start_join<kSinks>(c, a, s) : e;
+  }
+  if (p.wide > 0) {
+    if ((e = start_wide<kShared>(c, a, p, s)) != hipSuccess) return e;
+  } else {
+    a.stack_blocks = c.H * p.stack_parts * sc.n_groups * p.stack_tiles;
+  }
+  e = start<kShared>(c, a, p, s);
+  return e == hipSuccess ? start_join<kShared>(c, a, s) : e;
 }
 
 hipError_t launch_kv_shared_prefix(const KvDev& c, const int32_t* seqs, const int32_t* cu_rows, int n_groups,

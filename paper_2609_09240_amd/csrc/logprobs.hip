@@ -1,15 +1,16 @@
-// Log probabilities of rows of logits (gfx950), one pass over them:
-//     m = max x, S = sum exp(scale (x - m)), T = sum exp(scale (x - m)) (x - m),
-//     log p_j = scale (x_j - m) - log S,   H = log S - scale T / S,
-// with the sums rescaled whenever a thread's maximum grows (x - m <= 0, so
-// neither term of H cancels the other).
+// Log probabilities of rows of logits (gfx950), one pass over them.  With t_j =
+// scale log2(e) x_j - r, where r is a reference near the largest of them,
+//     S = sum 2^t_j,  T = sum 2^t_j t_j,
+//     log p_j = scale x_j - ln 2 (log2 S + r),   H = ln 2 (log2 S - T / S);
+// r moves, and the sums with it, whenever a thread's maximum grows.
 //
-// The most likely tokens.  A wave holds a chunk of 1024 logits in registers.  The
-// k-th largest of its 64 lanes' maxima bounds the k-th largest logit from below,
-// so that few others have to be looked at: those above the bound, and of those
-// equal to it the first k.  They go to LDS as whole numbers (order of the logit,
-// then of the index) and are ranked by counting.  In later chunks only what is
-// above the k-th so far is looked at, mostly nothing.
+// The most likely tokens.  A wave holds 1024 logits in registers.  The k-th
+// largest of its 64 lanes' maxima bounds the k-th largest logit from below, and
+// so does the largest such bound of the workgroup's waves: few logits reach it.
+// Those above it, and of those equal to it the first k of the wave, go to LDS as
+// whole numbers (order of the logit, then of the index), and are ranked by
+// counting, once for a workgroup.  In later chunks only what is above the bound is
+// looked at.
 //
 // A workgroup takes a row or, where there are few rows, a part of one; the last
 // workgroup of a row to leave its part joins them in their order.
@@ -19,14 +20,17 @@
 namespace tq {
 namespace {
 
-constexpr int kEach = 16, kThreads = 256, kChunk = kThreads * kEach;
+constexpr int kEach = 16, kThreads = 256, kWaves = kThreads / 64, kChunk = kThreads * kEach;
 constexpr int kMaxParts = 16, kMaxTop = TQ_LOGPROBS_MAX_TOP;
-constexpr int kPartFloats = 4 + 2 * kMaxTop;   // m, S, T, unused, keys
+constexpr int kPartFloats = 4 + 2 * kMaxTop;   // reference and its logit, S, T, keys
 constexpr int kWanted = 2048;                  // workgroups
-// Candidates of a wave: what it held, those above the bound in fewer than k
+// Candidates of a wave: what it held when a chunk began (ranked, and k left of
+// them, where it was more than kHeld), those above the bound in fewer than k
 // lanes, the first k equal to it.
-constexpr int kMost = kMaxTop + (kMaxTop - 1) * kEach + kMaxTop;
+constexpr int kHeld = 64, kMost = kHeld + (kMaxTop - 1) * kEach + kMaxTop;
+static_assert(kMaxParts * kMaxTop <= kMost && kMost % 8 == 0, "the join's keys, and ranking by eights");
 constexpr float kLowest = -3.4028234663852886e38f;   // of the finite numbers
+constexpr float kLn2 = 0.69314718055994531f;
 
 struct LogArgs {
   const void* x;
@@ -51,19 +55,39 @@ __device__ inline float logit_of(uint64_t key) {
   return __builtin_bit_cast(float, o ^ (o & 0x80000000u ? 0x80000000u : 0xFFFFFFFFu));
 }
 
+// A logit relative to a reference, in powers of two.  fp16 logits: x c - m c with
+// one rounding, where m c is rounded once for all of them, which changes
+// nothing but the reference.  fp32 logits may be as large as fp32 goes: (x - m) c.
+template <class T>
+struct Ref;
+template <>
+struct Ref<_Float16> {
+  float c, mc;
+  __device__ Ref(float m, float c) : c(c), mc(fmaxf(m, -65504.0f) * c) {
+    asm("" : "+v"(mc));   // rounded as it stands, into whatever sum it goes
+  }
+  __device__ float operator()(float x) const { return fmaf(x, c, -mc); }
+  __device__ float from(const Ref& o) const { return o.mc - mc; }   // of o's reference
+};
+template <>
+struct Ref<float> {
+  float c, m;
+  __device__ Ref(float m, float c) : c(c), m(fmaxf(m, kLowest)) {}
+  __device__ float operator()(float x) const { return (x - m) * c; }
+  __device__ float from(const Ref& o) const { return (o.m - m) * c; }
+};
+
+// Largest logit m, S and T against it.
 struct Sums {
   float m, s, t;
 };
+template <class T>
 __device__ inline Sums join(Sums a, Sums b, float c) {
-  Sums r;
-  r.m = fmaxf(a.m, b.m);
-  const float m = fmaxf(r.m, kLowest);
-  const float da = fmaxf(fmaxf(a.m, kLowest) - m, kLowest), db = fmaxf(fmaxf(b.m, kLowest) - m, kLowest);
-  const float fa = __builtin_amdgcn_exp2f(da * c), fb = __builtin_amdgcn_exp2f(db * c);
+  const Ref<T> ra(a.m, c), rb(b.m, c), r(fmaxf(a.m, b.m), c);
+  const float da = fmaxf(r.from(ra), kLowest), db = fmaxf(r.from(rb), kLowest);
+  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
   const float sa = a.s * fa, sb = b.s * fb;
-  r.s = sa + sb;
-  r.t = fmaf(sa, da, a.t * fa) + fmaf(sb, db, b.t * fb);
-  return r;
+  return Sums{fmaxf(a.m, b.m), sa + sb, fmaf(sa, da, a.t * fa) + fmaf(sb, db, b.t * fb)};
 }
 
 __device__ inline int below(uint64_t mask) {   // lanes of a mask before this one
@@ -76,42 +100,85 @@ __device__ inline void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The k-th largest of the 64 lanes' x (none of them NaN).
-__device__ inline float kth_of(float x, int k) {
-  int rank = 0;
-  const int lane = threadIdx.x & 63;
-#pragma unroll 8
-  for (int i = 0; i < 64; ++i) {
-    const float y = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
-    rank += y > x || (y == x && i < lane);
-  }
-  const int at = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(rank == k - 1)) - 1;
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), at));
+__device__ inline float lane_of(float x, int i) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
 }
 
-// The largest keys of a wave's part of a row, in LDS: `list` (n of them, the first k in
-// order between chunks), and what an unseen logit has to be above.
-struct Top {
-  uint64_t* list;
-  uint64_t* sorted;
-  int n;
-  float bound;
-};
+// One step of a sort of the lanes: of lanes whose numbers differ in bit J, the
+// one whose bit J is not that of the direction (bit K) takes the larger x.
+template <int J, int K>
+__device__ inline void sort_step(float& x, int lane) {
+  const int b = __builtin_bit_cast(int, x);
+  float y = x, z;
+  if constexpr (J >= 16) {   // both of a pair, in either lane
+    const auto w = J == 16 ? __builtin_amdgcn_permlane16_swap(b, b, false, false)
+                           : __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    y = __builtin_bit_cast(float, w[0]);
+    z = __builtin_bit_cast(float, w[1]);
+  } else if constexpr (J == 4) {   // lanes 4 up in the quads 0 and 2 of a row, 4 down in 1 and 3
+    const int w = __builtin_amdgcn_update_dpp(0, b, 0x104, 0xF, 0x5, false);
+    z = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(w, b, 0x114, 0xF, 0xA, false));
+  } else {   // quad_perm 1 0 3 2 and 2 3 0 1, row_ror 8
+    z = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, b, J == 1 ? 0xB1 : J == 2 ? 0x4E : 0x128, 0xF, 0xF, true));
+  }
+  const bool smaller = ((lane & J) != 0) != ((lane & K) != 0);
+  x = smaller ? fminf(y, z) : fmaxf(y, z);
+}
+template <int J, int K>
+__device__ inline void sort_steps(float& x, int lane) {
+  sort_step<J, K>(x, lane);
+  if constexpr (J > 1) sort_steps<J / 2, K>(x, lane);
+}
 
-__device__ inline void rank_keys(Top& top, int k) {
+// The k-th largest of the 64 lanes' x (none of them NaN): they are sorted, the
+// largest in lane 0.
+__device__ inline float kth_of(float x, int k) {
   const int lane = threadIdx.x & 63;
+  sort_steps<1, 2>(x, lane);
+  sort_steps<2, 4>(x, lane);
+  sort_steps<4, 8>(x, lane);
+  sort_steps<8, 16>(x, lane);
+  sort_steps<16, 32>(x, lane);
+  sort_steps<32, 64>(x, lane);
+  return lane_of(x, k - 1);
+}
+
+__device__ inline float wave_max(float x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+
+// Keys of a list of n, filled up with zeros to a multiple of 8, above one.
+__device__ inline int rank_in(const uint64_t* list, int n, uint64_t mine) {
+  int rank = 0;
+  for (int j = 0; j < n; j += 8) {
+    u4v w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = *reinterpret_cast<const u4v*>(&list[j + 2 * e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      rank += ((uint64_t)w[e][1] << 32 | w[e][0]) > mine;
+      rank += ((uint64_t)w[e][3] << 32 | w[e][2]) > mine;
+    }
+  }
+  return rank;
+}
+
+// The first k of a wave's n keys to the front of its list, in order; the rest
+// is gone.
+__device__ inline void rank_wave(uint64_t* list, uint64_t* sorted, int n, int k) {
+  const int lane = threadIdx.x & 63;
+  if (lane < 8 && n + lane < ((n + 7) & ~7)) list[n + lane] = 0;
   wave_sync();
-  for (int i = lane; i < top.n; i += 64) {
-    const uint64_t mine = top.list[i];
-    int rank = 0;
-    for (int j = 0; j < top.n; ++j) rank += top.list[j] > mine;
-    if (rank < k) top.sorted[rank] = mine;
+  for (int i = lane; i < n; i += 64) {
+    const uint64_t mine = list[i];
+    const int rank = rank_in(list, n, mine);
+    if (rank < k) sorted[rank] = mine;
   }
   wave_sync();
-  if (lane < k) top.list[lane] = top.sorted[lane];
+  if (lane < k) list[lane] = sorted[lane];
   wave_sync();
-  top.n = k;
-  top.bound = logit_of(top.list[k - 1]);
 }
 
 template <class T>
@@ -120,114 +187,173 @@ struct __attribute__((packed, aligned(sizeof(T)))) Vec {
 };
 
 template <class T, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(LogArgs a) {
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) logprobs_kernel(LogArgs a) {
   constexpr int VE = 16 / sizeof(T), NV = kEach / VE;
-  __shared__ uint64_t list[TOP ? kThreads / 64 : 1][TOP ? kMost : 1];
-  alignas(16) __shared__ uint64_t best[TOP ? kMaxParts * kMaxTop : 1];
-  __shared__ Sums sums[kThreads / 64];
+  alignas(16) __shared__ uint64_t list[TOP ? kWaves : 1][TOP ? kMost : 2];
+  __shared__ uint64_t best[TOP ? kMaxTop + 1 : 1], sorted[TOP ? kWaves : 1][TOP ? kMaxTop : 1];
+  __shared__ Sums sums[kWaves];
+  __shared__ float bounds[kWaves];
+  __shared__ int counts[kWaves + 1];
   __shared__ int last;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
   const T* x = static_cast<const T*>(a.x) + row * a.ld;
   const float c = a.scale * 1.4426950408889634f;
   const int k = TOP ? a.k : 0;
-  Sums z = {-__builtin_inff(), 0.0f, 0.0f};
-  Top top = {list[TOP ? wave : 0], best + (TOP ? wave * kMaxTop : 0), 0, -__builtin_inff()};
+  const float none = -__builtin_inff();
+  Sums z = {none, 0.0f, 0.0f};
+  uint64_t* mine = list[TOP ? wave : 0];
+  int held = 0;
+  float bound = none;
 
-  const int c0 = part * a.chunks;
-  for (int chunk = c0; chunk < c0 + a.chunks && chunk * kChunk < a.V; ++chunk) {
-    float v[kEach];
+  // Thread's logits of a chunk; past the row -infinity.
+  auto load = [&](Vec<T>(&w)[NV], int chunk) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int j = chunk * kChunk + (i * kThreads + tid) * VE;
       if (j + VE <= a.V) {
-        const Vec<T> w = *reinterpret_cast<const Vec<T>*>(x + j);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) v[i * VE + e] = (float)w.v[e];
+        w[i] = *reinterpret_cast<const Vec<T>*>(x + j);
       } else {
 #pragma unroll
-        for (int e = 0; e < VE; ++e) v[i * VE + e] = j + e < a.V ? (float)x[j + e] : -__builtin_inff();
+        for (int e = 0; e < VE; ++e) w[i].v[e] = j + e < a.V ? x[j + e] : (T)none;
       }
     }
-    float most = -__builtin_inff();
+  };
+  // The first k of n keys in list[0] to best, in order.
+  auto rank_all = [&](int n) {
+    if (tid < 8 && n + tid < ((n + 7) & ~7)) list[0][n + tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+      const uint64_t key = list[0][i];
+      const int rank = rank_in(list[0], n, key);
+      if (rank < k) best[rank] = key;
+    }
+    __syncthreads();
+  };
+  // The first k of all waves' keys to best, in order.
+  auto rank_lists = [&] {
+    if (held > kMost / kWaves) {   // all four lists fit one
+      rank_wave(mine, sorted[wave], held, k);
+      held = k;
+    }
+    if (lane == 0) counts[wave] = held;
+    __syncthreads();
+    int n = 0, at = 0;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) most = fmaxf(most, v[e]);
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) at += counts[w];
+      n += counts[w];
+    }
+    constexpr int kOwn = (kMost / kWaves + 63) / 64;
+    uint64_t key[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) key[i] = i * 64 + lane < held ? mine[i * 64 + lane] : 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (i * 64 + lane < held) list[0][at + i * 64 + lane] = key[i];
+    __syncthreads();
+    rank_all(n);
+  };
+  const int c0 = part * a.chunks, c1 = min(c0 + a.chunks, (a.V + kChunk - 1) / kChunk);
+  Vec<T> next[NV];
+  load(next, c0);
+  for (int chunk = c0; chunk < c1; ++chunk) {
+    Vec<T> w[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) w[i] = next[i];
+    if (chunk + 1 < c1) load(next, chunk + 1);
+    float v[kEach], most = none;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      v[e] = (float)w[e / VE].v[e % VE];
+      most = fmaxf(most, v[e]);
+    }
     {
-      const float now = fmaxf(z.m, most), m = fmaxf(now, kLowest), by = fmaxf(fmaxf(z.m, kLowest) - m, kLowest);
-      const float f = __builtin_amdgcn_exp2f(by * c);
-      z.s *= f;
-      if (ENTROPY) z.t = fmaf(z.s, by, z.t * f);
-      z.m = now;
+      const Ref<T> r(fmaxf(z.m, most), c);
+      if (most > z.m) {
+        const float by = fmaxf(r.from(Ref<T>(z.m, c)), kLowest), f = __builtin_amdgcn_exp2f(by);
+        z.s *= f;
+        if (ENTROPY) z.t = fmaf(z.s, by, z.t * f);
+        z.m = most;
+      }
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const float d = v[e] - m, p = __builtin_amdgcn_exp2f(d * c);
+        const float t = r(v[e]), p = __builtin_amdgcn_exp2f(t);
         z.s += p;
-        if (ENTROPY) z.t = fmaf(p, fmaxf(d, kLowest), z.t);   // 0 times -infinity
+        if (ENTROPY) z.t = fmaf(p, fmaxf(t, kLowest), z.t);   // 0 times -infinity
       }
     }
     if constexpr (TOP) {
       const bool first = chunk == c0;
-      const uint64_t above = __builtin_amdgcn_ballot_w64(most > top.bound);
-      if (!first && above == 0) continue;
-      const bool equal = first || __popcll(above) >= k;
-      if (equal) top.bound = kth_of(most, k);
-      int n = top.n;
+      bool equal = first;
+      if (first) {
+        const float b = k == 1 ? wave_max(most) : kth_of(most, k);
+        if (lane == 0) bounds[wave] = b;
+        __syncthreads();
+        bound = fmaxf(fmaxf(bounds[0], bounds[1]), fmaxf(bounds[2], bounds[3]));
+      } else {
+        const uint64_t above = __builtin_amdgcn_ballot_w64(most > bound);
+        if (above == 0) continue;
+        if (held > kHeld) {
+          rank_wave(mine, sorted[wave], held, k);
+          held = k;
+          bound = fmaxf(bound, logit_of(mine[k - 1]));
+        }
+        if (__popcll(above) >= k) {
+          const float b = kth_of(most, k);
+          equal = b > bound;
+          bound = fmaxf(bound, b);
+        }
+      }
+      // (Opaque: as one comparison with what follows the compiler keeps 16 masks.)
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(v[e] > top.bound);
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(v[e] > bound);
         if (mask == 0) continue;
         const int j = chunk * kChunk + (e / VE * kThreads + tid) * VE + e % VE;
-        if (v[e] > top.bound) top.list[n + below(mask)] = key_of(v[e], j);
-        n += __popcll(mask);
+        if (v[e] > bound) mine[held + below(mask)] = key_of(v[e], j);
+        held += __popcll(mask);
       }
       int ties = 0;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         if (!equal || ties >= k) break;
-        int mine = 0;
+        int n = 0;
         // (a NaN ranks as -infinity)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) mine += fmaxf(v[i * VE + e], -__builtin_inff()) == top.bound;
-        if (__builtin_amdgcn_ballot_w64(mine != 0) == 0) continue;
-        const int incl = wave_scan(mine);
-        int at = ties + incl - mine;
+        for (int e = 0; e < VE; ++e) n += fmaxf(v[i * VE + e], none) == bound;
+        if (__builtin_amdgcn_ballot_w64(n != 0) == 0) continue;
+        const int incl = wave_scan(n);
+        int at = ties + incl - n;
 #pragma unroll
         for (int e = 0; e < VE; ++e)
-          if (fmaxf(v[i * VE + e], -__builtin_inff()) == top.bound) {
-            if (at < k) top.list[n + at] = key_of(top.bound, chunk * kChunk + (i * kThreads + tid) * VE + e);
+          if (fmaxf(v[i * VE + e], none) == bound) {
+            if (at < k) mine[held + at] = key_of(bound, chunk * kChunk + (i * kThreads + tid) * VE + e);
             ++at;
           }
         ties += __builtin_amdgcn_readlane(incl, 63);
       }
-      top.n = n + min(ties, k);
-      rank_keys(top, k);
+      held += min(ties, k);
+      if (first && c1 > c0 + 1) {   // the bound of the whole chunk
+        rank_lists();
+        held = wave == 0 ? k : 0;
+        if (tid < k) list[0][tid] = best[tid];
+        bound = logit_of(best[k - 1]);
+        __syncthreads();
+      }
     }
   }
 
   // The workgroup's sums and keys.
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) z = join(z, Sums{__shfl_xor(z.m, d), __shfl_xor(z.s, d), __shfl_xor(z.t, d)}, c);
+  for (int d = 1; d < 64; d *= 2) z = join<T>(z, Sums{__shfl_xor(z.m, d), __shfl_xor(z.s, d), __shfl_xor(z.t, d)}, c);
   if (lane == 0) sums[wave] = z;
+  if constexpr (TOP) rank_lists();
   __syncthreads();
   z = sums[0];
 #pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) z = join(z, sums[w], c);
-  auto rank_all = [&](int n) {   // keys in list[0][0 .. n) to best[0 .. k), from largest
-    for (int i = tid; i < n; i += kThreads) {
-      const uint64_t mine = list[0][i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += list[0][j] > mine;
-      if (rank < k) best[rank] = mine;
-    }
-    __syncthreads();
-  };
-  if constexpr (TOP) {
-    const uint64_t mine = tid < 4 * k ? list[tid / k][tid % k] : 0;
-    __syncthreads();
-    if (tid < 4 * k) list[0][tid] = mine;
-    __syncthreads();
-    rank_all(4 * k);
-  }
+  for (int w = 1; w < kWaves; ++w) z = join<T>(z, sums[w], c);
 
   if (a.parts > 1) {
     const __amdgpu_buffer_rsrc_t parts_of =
@@ -236,7 +362,8 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogArgs a) {
     if (tid == 0) put4(parts_of, at, float4v{z.m, z.s, z.t, 0.0f});
     if constexpr (TOP)
       if (tid < (k + 1) / 2) {
-        const u4v w = *reinterpret_cast<const u4v*>(&best[2 * tid]);
+        const uint64_t p = best[2 * tid], q = best[2 * tid + 1];
+        const u4v w = {(uint32_t)p, (uint32_t)(p >> 32), (uint32_t)q, (uint32_t)(q >> 32)};
         put4(parts_of, at + 16 + 16 * tid, __builtin_bit_cast(float4v, w));
       }
     __builtin_amdgcn_s_waitcnt(0);   // what is joined has arrived
@@ -246,32 +373,51 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogArgs a) {
       if (before == a.parts - 1) __hip_atomic_store(a.count + row, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       last = before == a.parts - 1;
     }
+    if (tid <= kWaves) counts[tid] = 0;
     __syncthreads();
     if (!last) return;
     asm volatile("" ::: "memory");
     const int at0 = row * a.parts * kPartFloats * 4;
-    for (int p = 0; p < a.parts; ++p) {
-      const float4v w = get4(parts_of, at0 + p * kPartFloats * 4);
-      const Sums y = {w[0], w[1], w[2]};
-      z = p == 0 ? y : join(z, y, c);
-    }
+    // Lane p of every 16 has part p's sums.
+    const float4v w = get4(parts_of, at0 + min(lane & 15, a.parts - 1) * kPartFloats * 4);
+    z = (lane & 15) < a.parts ? Sums{w[0], w[1], w[2]} : Sums{none, 0.0f, 0.0f};
     if constexpr (TOP) {
-      const int pairs = (k + 1) / 2;
-      for (int i = tid; i < a.parts * pairs; i += kThreads) {
-        const int p = i / pairs, e = i - p * pairs;
-        const u4v w = __builtin_bit_cast(u4v, get4(parts_of, at0 + p * kPartFloats * 4 + 16 + 16 * e));
-        list[0][p * k + 2 * e] = (uint64_t)w[1] << 32 | w[0];
-        if (2 * e + 1 < k) list[0][p * k + 2 * e + 1] = (uint64_t)w[3] << 32 | w[2];
+      // Of every part's keys the n-th, with n parts >= k: at least k keys are not
+      // below the least of them.
+      const int pairs = (k + 1) / 2, nth = (k + a.parts - 1) / a.parts;
+      constexpr int kOwn = kMaxParts * kMaxTop / 2 / kThreads;
+      static_assert(kOwn == 1, "a pair of keys a thread");
+      uint64_t key[2] = {0, 0};
+      const int p = tid / pairs, e = tid - p * pairs;
+      if (p < a.parts) {
+        const u4v y = __builtin_bit_cast(u4v, get4(parts_of, at0 + p * kPartFloats * 4 + 16 + 16 * e));
+        key[0] = (uint64_t)y[1] << 32 | y[0];
+        if (2 * e + 1 < k) key[1] = (uint64_t)y[3] << 32 | y[2];
+        if ((nth - 1) / 2 == e) best[p] = key[(nth - 1) & 1];
       }
       __syncthreads();
-      rank_all(a.parts * k);
+      uint64_t least = best[0];
+      for (int i = 1; i < a.parts; ++i) least = best[i] < least ? best[i] : least;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(key[i] != 0 && key[i] >= least);
+        int first = 0;
+        if (lane == 0 && mask != 0) first = atomicAdd(&counts[kWaves], __popcll(mask));
+        first = __builtin_amdgcn_readfirstlane(first);
+        if (key[i] != 0 && key[i] >= least) list[0][first + below(mask)] = key[i];
+      }
+      __syncthreads();
+      rank_all(counts[kWaves]);
     }
+#pragma unroll
+    for (int d = 1; d < kMaxParts; d *= 2)
+      z = join<T>(z, Sums{__shfl_xor(z.m, d), __shfl_xor(z.s, d), __shfl_xor(z.t, d)}, c);
   }
 
   // What is asked for.  Where no token is possible S is 0.
-  const bool none = z.s == 0.0f;
-  const float log_s = logf(z.s);
-  auto logp = [&](float v) { return none ? -__builtin_inff() : (v - z.m) * a.scale - log_s; };
+  const bool empty = z.s == 0.0f;
+  const float log2_s = log2f(z.s), log_s = (log2_s - Ref<T>(z.m, c)(z.m)) * kLn2;   // against z.m itself
+  auto logp = [&](float v) { return empty ? none : (v - z.m) * a.scale - log_s; };
   for (int i = tid; i < a.n_ids; i += kThreads) {
     const int64_t at = (int64_t)row * a.n_ids + i;
     const int id = a.ids[at];
@@ -279,7 +425,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogArgs a) {
     a.logp[at] = in ? logp((float)x[id]) : __builtin_nanf("");
     if (!in && a.d_err != nullptr) atomicAdd(a.d_err, 1);
   }
-  if (ENTROPY && tid == 0) a.entropy[row] = none ? 0.0f : log_s - a.scale * z.t / z.s;
+  if (ENTROPY && tid == 0) a.entropy[row] = empty ? 0.0f : (log2_s - z.t / z.s) * kLn2;
   if constexpr (TOP) {
     if (tid < k) {
       const uint64_t key = best[tid];
@@ -289,13 +435,14 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(LogArgs a) {
   }
 }
 
-// Parts of a row, and chunks of one: as many workgroups as fill the chip, whole
-// chunks each.
+// Parts of a row, and chunks of one: as many workgroups as the chip holds at
+// once, two chunks each at least (the second is on its way while the first is
+// looked at; joining takes 3 us).
 void split(const tq_logprobs_call& c, int* parts, int* chunks) {
   const int all = (c.n_vocab + kChunk - 1) / kChunk;
-  int p = (kWanted + c.n_rows - 1) / c.n_rows;
-  p = p < all ? p : all;
-  p = p < kMaxParts ? p : kMaxParts;
+  int p = kWanted / c.n_rows;
+  p = p < all / 2 ? p : all / 2;
+  p = p < 1 ? 1 : p < kMaxParts ? p : kMaxParts;
   *chunks = (all + p - 1) / p;
   *parts = (all + *chunks - 1) / *chunks;
 }

@@ -12,6 +12,8 @@ from scope_helpers import Branches, check, i32
 
 pytestmark = pytest.mark.gpu
 
+FEW, MANY = dict(max_prefix=2000), dict(max_prefix=1 << 20)   # short caches attended together all the same, in few or many parts
+
 
 def run(m, q, nq, seqs, groups=None, prefix=None, f32=True, **kw):
     seqs_t = i32(*seqs)
@@ -35,9 +37,10 @@ def test_decode(D, G, share):
     m = Branches([170], [0] * 11, [1, 2, 31, 32, 33, 0, 64, 65, 100, 5, 1], 2, D, G, 32, seed=D + G)
     seqs = m.kids + [0]
     q = rows((12, 2 * share, D), 5)
-    o, lse = run(m, q, [1] * 12, seqs)
-    check(m, q, [1] * 12, o, lse, seqs=seqs)
-    h, _ = run(m, q, [1] * 12, seqs, f32=False)
+    for hint in (FEW, MANY, {}):
+        o, lse = run(m, q, [1] * 12, seqs, **hint)
+        check(m, q, [1] * 12, o, lse, seqs=seqs)
+    h, _ = run(m, q, [1] * 12, seqs, f32=False, **FEW)
     check(m, q, [1] * 12, h, lse, seqs=seqs, f32=False)
 
 
@@ -53,13 +56,14 @@ def test_groups_and_many_queries(D, G, H, share, ps):
     nq = [3, 40, 2, 0, 1, 60, 1, 1, 2, 7, 3, 1, 1, 5]
     groups = [0, 4, 7, 10, 10, 13, 14]
     q = rows((sum(nq), H * share, D), 6)
-    o, lse = run(m, q, nq, seqs, groups)
-    check(m, q, nq, o, lse, seqs=seqs)
+    for hint in (FEW, MANY, {}):
+        o, lse = run(m, q, nq, seqs, groups, **hint)
+        check(m, q, nq, o, lse, seqs=seqs)
     # rows whose prompts differ share nothing; queries past max_q are left alone
-    lone = run(m, q, nq, seqs, [0, 14])
+    lone = run(m, q, nq, seqs, [0, 14], **FEW)
     check(m, q, nq, *lone, seqs=seqs)
     o2 = torch.full_like(o, 9.0)
-    o2, lse2 = run(m, q, nq, seqs, groups, max_q=3, o=o2)
+    o2, lse2 = run(m, q, nq, seqs, groups, max_q=3, o=o2, **FEW)
     check(m, q, nq, o2, lse2, seqs=seqs, max_q=3)
     past = np.concatenate([np.arange(n) >= 3 for n in nq])
     assert bool((o2.cpu()[past] == 9).all())
@@ -97,19 +101,23 @@ def test_any_part_of_what_is_shared(prefix):
     q = rows((3, 8, 128), 9)
     if prefix > 128:                                         # past the pages that are shared: as many as are
         prefix = 128
-    o, lse = run(m, q, [1] * 3, m.kids, prefix=i32(*[prefix] * 3))
-    check(m, q, [1] * 3, o, lse, seqs=m.kids)
-    # one row keeps out
-    o, lse = run(m, q, [1] * 3, m.kids, prefix=i32(0, prefix, prefix))
-    check(m, q, [1] * 3, o, lse, seqs=m.kids)
+    for hint in (FEW, MANY):
+        o, lse = run(m, q, [1] * 3, m.kids, prefix=i32(*[prefix] * 3), **hint)
+        check(m, q, [1] * 3, o, lse, seqs=m.kids)
+        # one row keeps out
+        o, lse = run(m, q, [1] * 3, m.kids, prefix=i32(0, prefix, prefix), **hint)
+        check(m, q, [1] * 3, o, lse, seqs=m.kids)
 
 
 def test_a_query_inside_the_prefix_sees_its_past_only():
     """Rows whose last tokens are shared ones: nothing was added behind the fork."""
     m = Branches([128], [0, 0, 0], [0, 0, 3], 1, 64, 32, 32)
-    q = rows((21, 4, 64), 3)
-    o, lse = run(m, q, [10, 7, 4], m.kids)
-    check(m, q, [10, 7, 4], o, lse, seqs=m.kids)
+    q = rows((61, 4, 64), 3)
+    for hint in (FEW, MANY, {}):
+        for nq in ([10, 7, 4], [20, 1, 40]):                  # few rows beside each other, and many
+            n = sum(nq)
+            o, lse = run(m, q[:n], nq, m.kids, **hint)
+            check(m, q[:n], nq, o, lse, seqs=m.kids)
 
 
 def test_positions_without_a_page_and_poison():
@@ -119,7 +127,7 @@ def test_positions_without_a_page_and_poison():
     q = rows((2, 4, 64), 2)
     prefix = i32(128, 128)
     m.cache.pages[1:3, 1] = -1
-    o, lse = run(m, q, [1, 1], m.kids, prefix=prefix)
+    o, lse = run(m, q, [1, 1], m.kids, prefix=prefix, **FEW)
     keep = [np.r_[0:32, 64:n] for n in (133, 168)]
     for s, kp in zip((1, 2), keep):
         m.k[s], m.v[s] = m.k[s][kp], m.v[s][kp]
@@ -128,7 +136,7 @@ def test_positions_without_a_page_and_poison():
     bad = torch.full((1, 1, 64), float("nan"), dtype=torch.float16, device="cuda")
     m.cache.lens[0] = 128
     tq.tq_kv_append(m.cache, 0, bad, bad, i32(70), seqs=i32(0))        # a shared page
-    o2, _ = run(m, q, [1, 1], m.kids, prefix=prefix)
+    o2, _ = run(m, q, [1, 1], m.kids, prefix=prefix, **FEW)
     assert bool(torch.isnan(o2).any(-1).all())
 
 
@@ -162,8 +170,9 @@ def test_layers_strides_and_a_pool_past_4_gib():
     buf = torch.zeros((3, 48, 130), dtype=torch.float16, device="cuda")
     view = buf[:, 3:35, 1:129]
     view.copy_(torch.from_numpy(q))
-    o, lse = tq.tq_kv_attention(c, 1, view, prefix=tq.tq_kv_shared_prefix(c), out_f32=True, want_lse=True)
-    check(m, q, [1] * 3, o, lse)
+    for hint in (FEW, MANY, {}):
+        o, lse = tq.tq_kv_attention(c, 1, view, prefix=tq.tq_kv_shared_prefix(c), out_f32=True, want_lse=True, **hint)
+        check(m, q, [1] * 3, o, lse)
 
 
 def test_workspaces_streams_and_graphs():
@@ -277,7 +286,7 @@ def test_refusals():
             call(**kw)
         assert e.value.status == 2, kw
     with pytest.raises(tq.TqError) as e:
-        call(workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        call(workspace=torch.empty(16, dtype=torch.uint8, device="cuda"), **FEW)
     assert e.value.status == 2
     for kw in (dict(groups=i32(0, 1, 1, 2), seqs=seqs), dict(seqs=torch.zeros(70000, dtype=torch.int32, device="cuda"))):
         with pytest.raises(tq.TqError) as e:
