@@ -28,16 +28,38 @@ struct ScopePlan {
   size_t bytes;         // workspace behind the counts
 };
 
-// Parts of `recs` records of each of `ids` tiles and heads, and what they take (us):
-// a wave needs 1 us for a record where it is alone on its SIMD, and 0.6 where others
-// work there; joining parts takes `join`.
-double split(int64_t ids, int64_t recs, int waves, double join, int* parts) {
+// Records of each of `ids` tiles and heads.
+struct Work {
+  int64_t ids, recs;
+};
+
+// What a launch of workgroups of `waves` waves takes (us), where `a` and `b` are cut
+// into parts: 2.5 for what starts and ends a workgroup, 1 for a record of a wave
+// alone on its SIMD, 0.6 of a SIMD's time for each where several are.
+double cost(const KvDev& c, int waves, Work a, int parts_a, Work b, int parts_b) {
+  const int lds = waves * 16 * (c.D + 6) * 4, by_lds = 160 * 1024 / lds, by_waves = 4 * waves_of(c.D, c.G) / waves;
+  const int64_t slots = (int64_t)kCus * (by_lds < by_waves ? by_lds : by_waves), n = a.ids * parts_a + b.ids * parts_b;
+  const double resident = (double)(n < slots ? n : slots), load = resident * waves / (4 * kCus);
+  const double each = 0.6 * load > 1.0 ? 0.6 * load : 1.0;
+  const double recs_a = a.ids > 0 ? (double)(a.recs + parts_a * waves - 1) / (parts_a * waves) : 0.0;
+  const double recs_b = b.ids > 0 ? (double)(b.recs + parts_b * waves - 1) / (parts_b * waves) : 0.0;
+  // One round: the longest workgroup; several: what there is, evenly.
+  double recs = recs_a > recs_b ? recs_a : recs_b;
+  const int64_t rounds = (n + slots - 1) / slots;
+  if (rounds > 1) {
+    const double even = (recs_a * a.ids * parts_a + recs_b * b.ids * parts_b) / slots;
+    recs = recs > even ? recs : even;
+  }
+  return 2.5 * rounds + recs * each;
+}
+
+// The best parts of `a` beside `b`, in workgroups of `waves` waves; `join`: what
+// joining parts takes.  A part is a record a wave at least.
+double split(const KvDev& c, int waves, Work a, Work b, int parts_b, double join, int* parts) {
   double best = 1e30;
-  for (int n = 1; n <= kMaxParts; n += n < 4 ? 1 : n / 4) {
-    if (n > 1 && recs < 2 * (int64_t)waves * n) break;
-    const double load = (double)ids * n * waves / (4 * kCus), each = 0.6 * load > 1.0 ? 0.6 * load : 1.0;
-    const double t = (double)((recs + (int64_t)n * waves - 1) / ((int64_t)n * waves)) * each + (n > 1 ? join : 0.0);
-    if (t < 0.95 * best) {
+  for (int n = 1; n <= kMaxParts && (n == 1 || a.recs >= (int64_t)waves * n); n += n < 4 ? 1 : n / 4) {
+    const double t = cost(c, waves, a, n, b, parts_b) + (n > 1 ? join : 0.0);
+    if (t < best) {
       best = t;
       *parts = n;
     }
@@ -53,7 +75,7 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
   constexpr int64_t kMostIds = 1 << 23, kMostOfTwo = 1 << 21;
   p->plain = p->sinks = false;
   p->wide = p->stack_parts = p->stack_tiles = 0;
-  p->waves = c.D == 256 ? 4 : 8;
+  p->waves = 4;
   p->tiles = (int)tiles;
   p->bytes = 0;
   if (tiles > 65535 || ids > kMostIds) return false;
@@ -65,10 +87,22 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
     const int64_t stack_tiles = (stacked + 15) / 16, stack_ids = (stack_tiles + sc.n_groups) * c.H;
     if (stack_tiles <= 65535 && ids <= kMostOfTwo && stack_tiles * sc.n_groups * c.H <= kMostOfTwo) {
       p->stack_tiles = (int)stack_tiles;
-      const double t = split(stack_ids, prefix, p->waves, 0.0, &p->stack_parts) +
-                       0.5 * split(ids, tail, p->waves, 0.0, &p->parts) + 6.0;
+      const Work stack{stack_ids, prefix}, rest{ids, tail}, none{0, 0};
+      split(c, 4, rest, none, 1, 0.0, &p->parts);
+      double t = split(c, 4, stack, rest, p->parts, 0.0, &p->stack_parts);
+      p->waves = 4;
+      if (c.D != 256) {
+        int n;
+        const double t8 = split(c, 8, stack, rest, p->parts, 0.0, &n);
+        if (t8 < t) {
+          t = t8;
+          p->waves = 8;
+          p->stack_parts = n;
+        }
+      }
       int n;
-      const double alone = split(ids, prefix + tail, 4, 8.0, &n);
+      const double alone = split(c, 4, Work{ids, prefix + tail}, none, 1, 8.0, &n);
+      t += 6.0;   // the second launch
       if (t < alone) {
         if (of_group >= 48 && share <= 1024 && stack_ids * prefix > 60000) {
           p->wide = 1;
@@ -88,12 +122,13 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
   p->plain = !p->sinks;
   if (p->plain) return true;
   const int64_t most = (int64_t)a.window + a.max_q + sc.sinks + 31, len = hint < most ? hint : most;
-  int parts4;
-  const double t4 = split(ids, len / 32 + 1, 4, 6.0, &parts4);
-  const double t8 = split(ids, len / 32 + 1, 8, 6.0, &p->parts);
-  if (p->waves == 4 || t4 <= t8 || ids > kMostOfTwo || !joined) {
-    p->waves = 4;
-    p->parts = parts4;
+  const Work all{ids, len / 32 + 1}, none{0, 0};
+  int n;
+  p->waves = 4;
+  const double t = split(c, 4, all, none, 1, 6.0, &p->parts);
+  if (c.D != 256 && ids <= kMostOfTwo && split(c, 8, all, none, 1, 6.0, &n) < t) {
+    p->waves = 8;
+    p->parts = n;
   }
   if (!joined) p->parts = 1;
   if (p->parts > 1) p->bytes = (size_t)p->parts * part_bytes;
@@ -109,7 +144,7 @@ hipError_t start(const KvDev& c, const MoreArgs& a, const ScopePlan& p, hipStrea
         kv_attn_kernel<D(), G(), MODE, 8><<<grid, 64 * 8, 0, s>>>(a);
         return;
       }
-    if constexpr (D() == 256 || MODE == kSinks) kv_attn_kernel<D(), G(), MODE, 4><<<grid, 64 * 4, 0, s>>>(a);
+    kv_attn_kernel<D(), G(), MODE, 4><<<grid, 64 * 4, 0, s>>>(a);
   });
 }
 

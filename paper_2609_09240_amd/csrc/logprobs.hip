@@ -113,8 +113,9 @@ __device__ inline void sort_step(float& x, int lane) {
   if constexpr (J >= 16) {   // both of a pair, in either lane
     const auto w = J == 16 ? __builtin_amdgcn_permlane16_swap(b, b, false, false)
                            : __builtin_amdgcn_permlane32_swap(b, b, false, false);
-    y = __builtin_bit_cast(float, w[0]);
-    z = __builtin_bit_cast(float, w[1]);
+    const uint32_t w0 = w[0], w1 = w[1];   // (a bit cast of a vector's element takes its first one)
+    y = __builtin_bit_cast(float, w0);
+    z = __builtin_bit_cast(float, w1);
   } else if constexpr (J == 4) {   // lanes 4 up in the quads 0 and 2 of a row, 4 down in 1 and 3
     const int w = __builtin_amdgcn_update_dpp(0, b, 0x104, 0xF, 0x5, false);
     z = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(w, b, 0x114, 0xF, 0xA, false));

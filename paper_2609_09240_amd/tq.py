@@ -7,9 +7,9 @@ library's kernels.  There is no fallback: if libtq.so is missing, every call
 raises.
 """
 
-import contextlib
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -245,9 +245,9 @@ def lib():
                                                       ctypes.c_size_t),
             "tq_kv_attention_scope": ([cp, i32, ctypes.POINTER(TqKvAttn), ctypes.POINTER(TqKvScope), vp], ctypes.c_int),
             "tq_kv_shared_prefix": ([cp, vp, vp, i32, i32, vp, vp], ctypes.c_int),
-            "tq_rope": ([ctypes.POINTER(TqRopeCall), vp], ctypes.c_int),
-            "tq_logprobs_workspace_bytes": ([ctypes.POINTER(TqLogprobsCall)], ctypes.c_size_t),
-            "tq_logprobs": ([ctypes.POINTER(TqLogprobsCall), vp], ctypes.c_int),
+            "tq_rope": ([vp, vp], ctypes.c_int),
+            "tq_logprobs_workspace_bytes": ([vp], ctypes.c_size_t),
+            "tq_logprobs": ([vp, vp], ctypes.c_int),
         }
         for name, (args, res) in sigs.items():
             fn = getattr(L, name)
@@ -652,13 +652,18 @@ class _Workspaces:
         return ws
 
     def get(self, need, stream):
-        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-            if torch.cuda.is_current_stream_capturing():
-                return self._new(need)
-            key = _stream(stream)
-            ws = self.by_stream.get(key)
-            if ws is None or ws.numel() < need:
-                ws = self.by_stream[key] = self._new(need)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self._get(need, stream)
+        return self._get(need, None)
+
+    def _get(self, need, stream):
+        if torch.cuda.is_current_stream_capturing():
+            return self._new(need)
+        key = _stream(stream)
+        ws = self.by_stream.get(key)
+        if ws is None or ws.numel() < need:
+            ws = self.by_stream[key] = self._new(need)
         return ws
 
 
@@ -1026,13 +1031,14 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
         raise ValueError("without cu_q, q must have one token a row")
     max_q = _most(max_q, cu_q, T)
     _fits(layer | max_q | max_len | window | sinks | max_prefix | max_tail)
-    scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail) if sinks or prefix is not None or groups is not None else None
+    scope = None
+    if sinks or prefix is not None or groups is not None:
+        scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail)
     qr = _kv_rows(q, None, cache.head_dim, "q")
-    dtype = torch.float32 if out_f32 else torch.float16
     if o is None:
-        o = torch.empty((T, n_heads, D), dtype=dtype, device=q.device)
+        o = torch.empty((T, n_heads, D), dtype=torch.float32, device=q.device) if out_f32 else q.new_empty(q.shape)
     else:
-        _out_buffer(o, (T, n_heads, D), dtype, "o")
+        _out_buffer(o, (T, n_heads, D), torch.float32 if out_f32 else torch.float16, "o")
     if lse is None:
         if want_lse:
             lse = torch.empty((T, n_heads), dtype=torch.float32, device=q.device)
@@ -1041,21 +1047,23 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
     a = TqKvAttn(n, T, max_q, n_heads, max_len, window, D ** -0.5 if scale is None else scale,
                  OUT_FP32 if out_f32 else OUT_FP16, _i32(seqs, n, "seqs"), _i32(cu_q, n + 1, "cu_q"), qr,
                  o.data_ptr(), None if lse is None else lse.data_ptr(), None, 0)
+    L = lib()
     if scope is None:
-        need = lib().tq_kv_attention_workspace_bytes(cache._ref, a)
+        need = L.tq_kv_attention_workspace_bytes(cache._ref, a)
     else:
-        need = lib().tq_kv_attention_scope_workspace_bytes(cache._ref, a, scope)
+        need = L.tq_kv_attention_scope_workspace_bytes(cache._ref, a, scope)
     if need:
         if workspace is None:
-            workspace = cache.attention_workspace(need, stream)
+            workspace = cache._ws.get(need, stream)
         else:
             _cuda(workspace, torch.uint8, "workspace")
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
     if scope is None:
-        _check(lib().tq_kv_attention(cache._ref, layer, a, _stream(stream)), "tq_kv_attention")
+        _check(L.tq_kv_attention(cache._ref, layer, a, _stream(stream)), "tq_kv_attention")
     else:
-        _check(lib().tq_kv_attention_scope(cache._ref, layer, a, scope, _stream(stream)), "tq_kv_attention_scope")
-    _used_on(stream, q, seqs, cu_q, o, lse, workspace, prefix, groups, *cache._buffers())
+        _check(L.tq_kv_attention_scope(cache._ref, layer, a, scope, _stream(stream)), "tq_kv_attention_scope")
+    if stream is not None:
+        _used_on(stream, q, seqs, cu_q, o, lse, workspace, prefix, groups, *cache._buffers())
     return (o, lse) if lse is not None else o
 
 
@@ -1063,11 +1071,20 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
 # Rotary positions and log probabilities.
 # --------------------------------------------------------------------------
 
-def _heads(t, d, name):
-    """fp16 [T, heads, D] on the GPU as tq_kv_rows, any strides but the last."""
-    if not (t.is_cuda and t.dtype == torch.float16 and t.dim() == 3 and t.shape[2] == d and t.stride(2) == 1):
-        raise ValueError(f"{name} must be float16 [tokens, heads, {d}] on the GPU with adjacent channels")
-    return TqKvRows(t.data_ptr(), t.stride(0), t.stride(1))
+# tq_rope_call and tq_logprobs_call as bytes: building a ctypes structure of as
+# many members takes 2 us more.
+_ROPE_CALL = struct.Struct("@7ifPqPP" + 4 * "Pqq")
+_LOGPROBS_CALL = struct.Struct("@5ifPq7PN")
+
+
+def _heads(t, shape, name):
+    """Address and strides of fp16 [T, heads, D] on the GPU, any strides but the last."""
+    if t.dtype is not torch.float16 or not t.is_cuda or t.shape != shape:
+        raise ValueError(f"{name} must be float16 {list(shape)} on the GPU")
+    ts, hs, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name} must have adjacent channels")
+    return t.data_ptr(), ts, hs
 
 
 def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, scale=1.0, q_out=None, k_out=None,
@@ -1080,38 +1097,43 @@ def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, sca
     the other way, which is also the gradient.  q_out and k_out: new tensors
     without; q and k themselves for a call in place.  Returns (q_out, k_out),
     q_out alone without k."""
-    if q.dim() != 3:
+    shape = q.shape
+    if len(shape) != 3:
         raise ValueError("q must be float16 [tokens, heads, D]")
-    T, n_heads, D = q.shape
-    if positions.dim() not in (1, 2) or positions.shape[-1] != T or positions.dtype != torch.int32 or \
-            not positions.is_cuda or (T > 1 and positions.stride(-1) != 1):
+    T, n_heads, D = shape
+    at = positions.shape
+    if len(at) not in (1, 2) or at[-1] != T or positions.dtype is not torch.int32 or not positions.is_cuda or \
+            (T > 1 and positions.stride(-1) != 1):
         raise ValueError("positions must be int32 [tokens] or [axes, tokens] on the GPU")
-    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    axes = 1 if len(at) == 1 else at[0]
     _cuda(freq, torch.float32, "freq")
+    n = freq.numel()
     if axis is not None:
         _cuda(axis, torch.uint8, "axis")
-        if axis.numel() != freq.numel():
+        if axis.numel() != n:
             raise ValueError("axis must name one for every frequency")
     elif axes > 1:
         raise ValueError("several axes need axis")
-    if k is not None and (k.dim() != 3 or k.shape[0] != T):
-        raise ValueError("k must be float16 [tokens, heads, D]")
+    qr = _heads(q, shape, "q")
     if q_out is None:
-        q_out = torch.empty((T, n_heads, D), dtype=torch.float16, device=q.device)
-    elif q_out.shape != q.shape:
-        raise ValueError("q_out must have the shape of q")
-    none = TqKvRows(None, 0, 0)
-    kr = ko = none
+        q_out = q.new_empty(shape)
+        qo = (q_out.data_ptr(), n_heads * D, D)
+    else:
+        qo = _heads(q_out, shape, "q_out")
+    kr = ko = (0, 0, 0)
+    kv_heads = 0
     if k is not None:
+        kv_heads = k.shape[1] if k.dim() == 3 else 0
+        kr = _heads(k, (T, kv_heads, D), "k")
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=torch.float16, device=q.device)
-        elif k_out.shape != k.shape:
-            raise ValueError("k_out must have the shape of k")
-        kr, ko = _heads(k, D, "k"), _heads(k_out, D, "k_out")
-    call = TqRopeCall(T, n_heads, 0 if k is None else k.shape[1], D, 2 * freq.numel(), axes,
-                      (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0), scale, positions.data_ptr(),
-                      0 if axes == 1 else positions.stride(0), freq.data_ptr(), _ptr(axis), _heads(q, D, "q"), kr,
-                      _heads(q_out, D, "q_out"), ko)
+            k_out = k.new_empty(k.shape)
+            ko = (k_out.data_ptr(), kv_heads * D, D)
+        else:
+            ko = _heads(k_out, k.shape, "k_out")
+    call = _ROPE_CALL.pack(T, n_heads, kv_heads, D, 2 * n, axes,
+                           (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0), scale,
+                           positions.data_ptr(), 0 if axes == 1 else positions.stride(0), freq.data_ptr(),
+                           0 if axis is None else axis.data_ptr(), *qr, *kr, *qo, *ko)
     _check(lib().tq_rope(call, _stream(stream)), "tq_rope")
     if stream is not None:
         _used_on(stream, q, k, positions, freq, axis, q_out, k_out)
@@ -1124,8 +1146,8 @@ _logprobs_ws = {}   # by device: workspaces of calls that bring none, one per st
 def tq_logprobs_workspace_bytes(n_rows, n_vocab, n_ids=1, n_top=0):
     """Workspace of tq_logprobs, 0 where it uses none."""
     _fits(n_rows | n_vocab | n_ids | n_top)
-    return int(lib().tq_logprobs_workspace_bytes(TqLogprobsCall(n_rows, n_vocab, n_ids, n_top, LOGITS_FP16, 1.0, None,
-                                                                n_vocab)))
+    return int(lib().tq_logprobs_workspace_bytes(
+        _LOGPROBS_CALL.pack(n_rows, n_vocab, n_ids, n_top, LOGITS_FP16, 1.0, 0, n_vocab, *(0,) * 8)))
 
 
 def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=None, workspace=None, stream=None):
@@ -1137,12 +1159,14 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
     was not asked for.  A token outside the vocabulary gets NaN and counts in
     d_err.  A workspace of the caller's has zeros in its first
     WORKSPACE_COUNT_BYTES before its first call."""
-    if not (logits.is_cuda and logits.dim() == 2 and logits.dtype in (torch.float16, torch.float32) and
-            (logits.stride(1) == 1 or logits.shape[1] == 1)):
-        raise ValueError("logits must be a float16 or float32 matrix on the GPU with adjacent elements in a row")
-    T, V = logits.shape
+    shape = logits.shape
+    if len(shape) != 2 or logits.dtype not in (torch.float16, torch.float32) or not logits.is_cuda:
+        raise ValueError("logits must be a float16 or float32 matrix on the GPU")
+    T, V = shape
+    ld, one = logits.stride()
+    if one != 1 and V != 1:
+        raise ValueError("logits must have adjacent elements in a row")
     _fits(T | V | top)
-    f32 = dict(dtype=torch.float32, device=logits.device)
     logp = entropy = top_ids = top_logp = None
     m = 0
     if ids is not None:
@@ -1150,16 +1174,18 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
         if ids.dim() not in (1, 2) or ids.shape[0] != T:
             raise ValueError("ids must be int32 [T] or [T, m]")
         m = 1 if ids.dim() == 1 else ids.shape[1]
-        logp = torch.empty(ids.shape, **f32)
+        logp = ids.new_empty(ids.shape, dtype=torch.float32)
     if want_entropy:
-        entropy = torch.empty(T, **f32)
-    if top:
-        top_ids = torch.empty((T, max(top, 0)), dtype=torch.int32, device=logits.device)
-        top_logp = torch.empty((T, max(top, 0)), **f32)
-    call = TqLogprobsCall(T, V, m, top, LOGITS_FP32 if logits.dtype == torch.float32 else LOGITS_FP16, scale,
-                          logits.data_ptr(), logits.stride(0) if T > 1 else V, _ptr(ids), _ptr(logp), _ptr(entropy),
-                          _ptr(top_ids), _ptr(top_logp), _i32(d_err, 1, "d_err"))
-    need = lib().tq_logprobs_workspace_bytes(call)
+        entropy = logits.new_empty(T, dtype=torch.float32)
+    if top > 0:
+        top_ids = logits.new_empty((T, top), dtype=torch.int32)
+        top_logp = logits.new_empty((T, top), dtype=torch.float32)
+    members = [T, V, m, top, LOGITS_FP32 if logits.dtype is torch.float32 else LOGITS_FP16, scale, logits.data_ptr(),
+               ld if T > 1 else V, *[0 if t is None else t.data_ptr() for t in (ids, logp, entropy, top_ids, top_logp)],
+               _i32(d_err, 1, "d_err") or 0, 0, 0]
+    L = lib()
+    call = _LOGPROBS_CALL.pack(*members)
+    need = L.tq_logprobs_workspace_bytes(call)
     if need:
         if workspace is None:
             ws = _logprobs_ws.get(logits.device)
@@ -1168,8 +1194,9 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
             workspace = ws.get(need, stream)
         else:
             _cuda(workspace, torch.uint8, "workspace")
-        call.workspace, call.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(lib().tq_logprobs(call, _stream(stream)), "tq_logprobs")
+        members[-2:] = workspace.data_ptr(), workspace.numel()
+        call = _LOGPROBS_CALL.pack(*members)
+    _check(L.tq_logprobs(call, _stream(stream)), "tq_logprobs")
     if stream is not None:
         _used_on(stream, logits, ids, logp, entropy, top_ids, top_logp, d_err, workspace)
     return logp, entropy, top_ids, top_logp

@@ -78,6 +78,14 @@ def test_sizes(f32, T, V):
         check(x, run(x, ids, top=top), ids, top)
 
 
+@pytest.mark.parametrize("T,V", [(40, 4096), (3, 9000), (2, 131072)])
+def test_every_number_of_tokens(T, V):
+    x = logits(T, V, 13, V != 9000)
+    order = decode.logprobs(x, None, 32)[2]
+    for top in range(1, 33):
+        np.testing.assert_array_equal(run(x, top=top)[2].cpu().numpy(), order[:, :top])
+
+
 @pytest.mark.parametrize("f32", [False, True])
 @pytest.mark.parametrize("scale", [1.0, 0.3, 7.5])
 def test_masks_ties_and_scales(f32, scale):
