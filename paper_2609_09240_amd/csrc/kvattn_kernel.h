@@ -220,9 +220,8 @@ __device__ inline int shared_of(const MoreArgs& a, int row) {
   return (int)min(max((int64_t)as_table(a.prefix)[row], (int64_t)0), most) & ~31;
 }
 
-// Tile qt (of R rows) of group g, whose pages are those of its first row that
-// shares any; false where there is none.
-template <int R>
+// Tile qt of group g, whose pages are those of its first row that shares any; false
+// where there is none.
 __device__ inline bool stack_of(const MoreArgs& a, int g, int qt, Tile* t) {
   const int r0 = a.cu_rows ? as_table(a.cu_rows)[g] : 0, r1 = a.cu_rows ? as_table(a.cu_rows)[g + 1] : a.n_rows;
   if (r0 < 0 || r1 > a.n_rows) return false;
@@ -239,7 +238,7 @@ __device__ inline bool stack_of(const MoreArgs& a, int g, int qt, Tile* t) {
   t->n = first < 0 || end <= first ? 0 : end - first;
   t->asked = t->n;
   t->rows = t->n * a.share;
-  t->row0 = qt * R;
+  t->row0 = qt * 16;
   if (t->row0 >= t->rows) return false;
   t->tok0 = qt == 0 ? 0 : t->row0 / a.share;
   t->head0 = t->row0 - t->tok0 * a.share;
@@ -274,8 +273,8 @@ __device__ inline int stack_pos(const MoreArgs& a, int b, int b1, int at) {
   return (int)max(min((int64_t)shared, len - asked + i + 1), (int64_t)0) - 1;
 }
 
-// Tile (b, qt) of R rows of head 0; false where there is none.
-template <int MODE, int R = 16, class A>
+// Tile (b, qt) of head 0; false where there is none.
+template <int MODE, class A>
 __device__ inline bool tile_of(const A& a, int b, int qt, Tile* t) {
   t->h = 0;
   t->b = b;
@@ -288,14 +287,14 @@ __device__ inline bool tile_of(const A& a, int b, int qt, Tile* t) {
   t->first = (int)first;
   t->n = bad || end <= first ? 0 : (int)(end - first);
   t->rows = t->n * a.share;
-  t->row0 = qt * R;
+  t->row0 = qt * 16;
   if (t->row0 >= t->rows) return false;
   t->tok0 = qt == 0 ? 0 : t->row0 / a.share;
   t->head0 = t->row0 - t->tok0 * a.share;
   t->len = length_of(a, t->seq);
   // Position of query token i is base + i; all of what was asked for counts.
   const int64_t base = t->len - asked;
-  const int last = min(t->tok0 + by_share(a, t->head0 + R - 1), t->n - 1);
+  const int last = min(t->tok0 + by_share(a, t->head0 + 15), t->n - 1);
   const int64_t hi = min((int64_t)t->len, base + last + 1);
   int64_t lo = a.window > 0 ? max((int64_t)0, base + t->tok0 + 1 - a.window) : 0;
   if constexpr (MODE == kShared) lo = t->shared = shared_of(a, b);
@@ -455,7 +454,7 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
     const int parts = stacked ? a.stack_parts : a.parts, n = stacked ? a.n_groups : a.n_rows;
     const int i = id / a.H, j = i / parts, qt = j / n;
     part = i - j * parts;
-    if (!(stacked ? stack_of<16>(a, j - qt * n, qt, &t) : tile_of<MODE>(a, j - qt * n, qt, &t))) return;
+    if (!(stacked ? stack_of(a, j - qt * n, qt, &t) : tile_of<MODE>(a, j - qt * n, qt, &t))) return;
     t.h = id - i * a.H;
     const int64_t all = t.rec1 - t.rec0;
     rec0 = t.rec0 + (int)(all * part / parts);

@@ -14,7 +14,6 @@
 
 #include "decode_internal.h"
 #include "kvattn_kernel.h"
-#include "kvwide.h"
 
 namespace tq {
 namespace {
@@ -24,7 +23,6 @@ struct ScopePlan {
   int waves;            // of a workgroup of kv_attn_kernel
   int tiles, parts;     // of a row, 16 query rows each; of its own tokens
   int stack_tiles, stack_parts;   // of a group
-  int wide;             // kv_wide_kernel for the stacked (or all) rows, with so many tiles of 16 rows a wave; 0: not
   size_t bytes;         // workspace behind the counts
 };
 
@@ -74,14 +72,14 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
   // What a grid holds: with 256 threads a workgroup, and with 512 of two kinds.
   constexpr int64_t kMostIds = 1 << 23, kMostOfTwo = 1 << 21;
   p->plain = p->sinks = false;
-  p->wide = p->stack_parts = p->stack_tiles = 0;
+  p->stack_parts = p->stack_tiles = 0;
   p->waves = 4;
   p->tiles = (int)tiles;
   p->bytes = 0;
   if (tiles > 65535 || ids > kMostIds) return false;
   const bool joined = a.max_q <= 65535;   // a grid of rows and tokens
   if (sc.n_groups > 0 && a.window == 0 && joined) {
-    const int64_t stacked = (int64_t)a.n_tokens * share, of_group = stacked / sc.n_groups;
+    const int64_t stacked = (int64_t)a.n_tokens * share;
     const int64_t prefix = (sc.max_prefix > 0 ? sc.max_prefix : hint) / 32;
     const int64_t tail = (sc.max_tail > 0 ? (int64_t)sc.max_tail + 31 : hint) / 32 + 1;
     const int64_t stack_tiles = (stacked + 15) / 16, stack_ids = (stack_tiles + sc.n_groups) * c.H;
@@ -104,14 +102,6 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
       const double alone = split(c, 4, Work{ids, prefix + tail}, none, 1, 8.0, &n);
       t += 6.0;   // the second launch
       if (t < alone) {
-        if (of_group >= 48 && share <= 1024 && stack_ids * prefix > 60000) {
-          p->wide = 1;
-          const int64_t n = (stacked + 63) / 64 + sc.n_groups;
-          p->stack_tiles = (int)((stacked + 63) / 64);
-          int64_t q = (3 * kCus + n * c.H - 1) / (n * c.H);
-          q = q < prefix / 8 ? q : prefix / 8;
-          p->stack_parts = (int)(q < 1 ? 1 : q < kMaxParts ? q : kMaxParts);
-        }
         p->bytes = (size_t)(p->parts + p->stack_parts) * part_bytes;
         return true;
       }
@@ -145,16 +135,6 @@ hipError_t start(const KvDev& c, const MoreArgs& a, const ScopePlan& p, hipStrea
         return;
       }
     kv_attn_kernel<D(), G(), MODE, 4><<<grid, 64 * 4, 0, s>>>(a);
-  });
-}
-
-template <int MODE>
-hipError_t start_wide(const KvDev& c, const MoreArgs& a, const ScopePlan& p, hipStream_t s) {
-  return with_sizes(c, [&](auto D, auto G) {
-    if constexpr (MODE == kShared) {
-      const dim3 grid(a.H * a.stack_parts, a.n_groups, p.stack_tiles);
-      kv_wide_kernel<D(), G(), MODE, 1><<<grid, 256, 0, s>>>(a);
-    }
   });
 }
 
@@ -255,11 +235,7 @@ hipError_t launch_kv_attention_scope(const KvDev& c, int layer, const AttnCall& 
     e = start<kSinks>(c, a, p, s);
     return e == hipSuccess && p.parts > 1 ? start_join<kSinks>(c, a, s) : e;
   }
-  if (p.wide > 0) {
-    if ((e = start_wide<kShared>(c, a, p, s)) != hipSuccess) return e;
-  } else {
-    a.stack_blocks = c.H * p.stack_parts * sc.n_groups * p.stack_tiles;
-  }
+  a.stack_blocks = c.H * p.stack_parts * sc.n_groups * p.stack_tiles;
   e = start<kShared>(c, a, p, s);
   return e == hipSuccess ? start_join<kShared>(c, a, s) : e;
 }
