@@ -5,10 +5,11 @@ in 4 bits, and a 4-bit output head.
 
 A small decoder with random weights (RMS norm, rotary positions, grouped
 heads, SwiGLU) reads a prompt, is forked into branches that share the
-prompt's pages, decodes each of them for a while, keeps the most likely one,
-gives the others' pages back, compacts the pool and goes on, at one row, from
-a HIP graph.  The projections are quantised by ``quantize_linear``; norms,
-rotations and the activation are a few lines of torch.
+prompt's pages, decodes each of them for a while (the pages that they share are
+attended once for all of them), keeps the most likely one, gives the others'
+pages back, compacts the pool and goes on, at one row, from a HIP graph.  The
+projections are quantised by ``quantize_linear``; norms and the activation are a
+few lines of torch.
 """
 
 import argparse
@@ -48,13 +49,6 @@ class Decoder:
         x = x.float()
         return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)).to(torch.float16)
 
-    def rotate(self, x, pos):
-        """Rotary positions on x [T, heads, D]."""
-        a = (pos.float()[:, None] * self.freq)[:, None]
-        c, s = torch.cos(a), torch.sin(a)
-        x1, x2 = x.float().chunk(2, -1)
-        return torch.cat([x1 * c - x2 * s, x2 * c + x1 * s], -1).to(torch.float16)
-
     @staticmethod
     def project(mats, x):
         """x W^T for matrices that read the same x [T, K]."""
@@ -66,8 +60,8 @@ class Decoder:
         """One decoder layer on x [T, hidden]; q_of attends: (layer, q) -> o."""
         T = x.shape[0]
         q, k, v = self.project([w["q"], w["k"], w["v"]], self.norm(x))
-        q = self.rotate(q.view(T, self.heads, self.d), pos)
-        k = self.rotate(k.view(T, self.kv_heads, self.d), pos)
+        q, k = q.view(T, self.heads, self.d), k.view(T, self.kv_heads, self.d)
+        tq.tq_rope(q, k, pos, self.freq, q_out=q, k_out=k)
         tq.tq_kv_append(self.cache, i, k, v.view(T, self.kv_heads, self.d), starts, seqs=seqs, cu_new=cu,
                         max_new=max_new)
         x = x + self.project([w["o"]], q_of(i, q).view(T, -1))[0]
@@ -75,19 +69,21 @@ class Decoder:
         act = (torch.nn.functional.silu(gate.float()) * up.float()).to(torch.float16)
         return x + self.project([w["down"]], act)[0]
 
-    def step(self, tokens, seqs, new=None, workspace=None):
+    def step(self, tokens, seqs, new=None, workspace=None, prefix=None):
         """Logits [rows, vocab] after new tokens [T] of slots `seqs`: one token a
-        row, or new[i] of them (a list).  T is at most 64."""
+        row, or new[i] of them (a list).  T is at most 64.  prefix: the first
+        tokens that the slots have in the same pages."""
         rows = seqs.numel()
         cu = None
         if new is not None:
             cu = torch.tensor([0, *torch.tensor(new).cumsum(0).tolist()], dtype=torch.int32, device="cuda")
         starts = tq.tq_kv_extend(self.cache, cu_new=cu, seqs=seqs)
-        pos = starts if cu is None else torch.cat([starts[i] + torch.arange(n, device="cuda") for i, n in enumerate(new)])
+        pos = starts if cu is None else torch.cat(
+            [starts[i] + torch.arange(n, dtype=torch.int32, device="cuda") for i, n in enumerate(new)])
 
         def attend(i, q):
             return tq.tq_kv_attention(self.cache, i, q, seqs=seqs, cu_q=cu, max_q=1 if new is None else max(new),
-                                      max_len=self.max_len, workspace=workspace)
+                                      max_len=self.max_len, workspace=workspace, prefix=prefix)
 
         x = self.embed[tokens]
         for i, w in enumerate(self.layers):
@@ -115,13 +111,14 @@ def generate(layers=2, branches=3, tokens=24, seed=0, log=print):
     tq.tq_kv_fork(m.cache, slots(*[0] * branches), kids)
     tq.tq_kv_free(m.cache, slots(0))
     log(f"{branches} branches: {int((m.cache.refs > 0).sum())} pages, {int((m.cache.refs > 1).sum())} of them shared")
-    nxt = torch.topk(logits[0], branches).indices
-    logp = torch.log_softmax(logits[0], -1)[nxt]
-    out = [[int(t)] for t in nxt]
+    shared = tq.tq_kv_shared_prefix(m.cache, seqs=kids)
+    _, _, ids, logp = tq.tq_logprobs(logits, top=branches)
+    nxt, logp = ids[0], logp[0]
+    out = [[t] for t in nxt.tolist()]
     for _ in range(tokens // 2):
-        logits = m.step(nxt, kids)
-        best = torch.log_softmax(logits, -1).max(-1)
-        nxt, logp = best.indices, logp + best.values
+        logits = m.step(nxt, kids, prefix=shared)
+        _, _, ids, best = tq.tq_logprobs(logits, top=1)
+        nxt, logp = ids[:, 0], logp + best[:, 0]
         for o, t in zip(out, nxt.tolist()):
             o.append(t)
 
@@ -137,15 +134,20 @@ def generate(layers=2, branches=3, tokens=24, seed=0, log=print):
     # One row from here on: the step as a graph, its token and logits in place.
     seq, tok, kept = kids[keep:keep + 1].clone(), nxt[keep:keep + 1].clone(), out[keep]
     ws = m.cache.attention_workspace(tq.tq_kv_attention_workspace_bytes(m.cache, 1, m.heads, max_len=m.max_len))
+    ws_top = torch.zeros(tq.tq_logprobs_workspace_bytes(1, m.vocab, n_ids=0, n_top=1), dtype=torch.uint8, device="cuda")
+
+    def most_likely(logits):
+        return tq.tq_logprobs(logits, top=1, workspace=ws_top)[2][0]
+
     left = tokens - tokens // 2
     # (A first step outside of the graph; it counts.)
-    tok.copy_(m.step(tok, seq, workspace=ws).argmax(-1))
+    tok.copy_(most_likely(m.step(tok, seq, workspace=ws)))
     kept.append(int(tok))
     graph = torch.cuda.CUDAGraph()
     torch.cuda.synchronize()
     with torch.cuda.graph(graph):
         logits = m.step(tok, seq, workspace=ws)
-        tok.copy_(logits.argmax(-1))
+        tok.copy_(most_likely(logits))
     for _ in range(left - 1):
         graph.replay()
         kept.append(int(tok))
