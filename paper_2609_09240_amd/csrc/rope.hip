@@ -2,11 +2,13 @@
 // token's position on the pair's axis,
 //     (x1, x2) -> scale (x1 cos a - x2 sin a, x2 cos a + x1 sin a).
 //
-// Bound by memory: every channel is read and written once.  A thread takes V
-// pairs of one token for several heads, so that its V angles are formed once
-// for them.  An angle is a product in 64 bits, reduced to a fraction of a turn
-// there (what a position of 10^6 leaves of a product in 32 bits is 0.06), then
-// sine and cosine in 32 bits.
+// Bound by memory: every channel is read and written once (8191 tokens of 32 + 8
+// heads of 128, 168 MB: 35 us, 4.8 TB/s).  A thread takes V pairs of one token for
+// several heads, so that its V angles are formed once for them: formed for every
+// two heads they take 55 us.  Four heads are loaded at a time, 8 or 10 are no
+// faster.  An angle is a product in 64 bits, reduced to a fraction of a turn there
+// (what a position of 10^6 leaves of a product in 32 bits is 0.06), then sine and
+// cosine in 32 bits.
 
 #include "decode_internal.h"
 
@@ -22,7 +24,7 @@ struct RopeArgs {
   int64_t axis_stride, q_ts, q_hs, k_ts, k_hs, qo_ts, qo_hs, ko_ts, ko_hs;
   int32_t n_tokens, n_heads, heads, half, rot, n_axes;
   int32_t turning, units;   // threads of a token that turn V pairs each, and with those that copy V channels
-  int32_t tokens;           // of a workgroup
+  int32_t tokens, per;      // of a workgroup, and heads
   float scale, sign;
 };
 
@@ -36,24 +38,17 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
   const int tl = threadIdx.x / a.units, u = threadIdx.x - tl * a.units + 256 * blockIdx.z;
   const int64_t t = (int64_t)blockIdx.x * a.tokens + tl;
   if (tl >= a.tokens || u >= a.units || t >= a.n_tokens) return;
-  const int h0 = blockIdx.y * HEADS, h1 = min(h0 + HEADS, a.heads);
+  const int from_head = blockIdx.y * a.per, to_head = min(from_head + a.per, a.heads);
   auto from = [&](int h) { return h < a.n_heads ? a.q + t * a.q_ts + h * a.q_hs : a.k + t * a.k_ts + (h - a.n_heads) * a.k_hs; };
   auto to = [&](int h) { return h < a.n_heads ? a.qo + t * a.qo_ts + h * a.qo_hs : a.ko + t * a.ko_ts + (h - a.n_heads) * a.ko_hs; };
   if (u >= a.turning) {
     const int d = a.rot + (u - a.turning) * V;
-    for (int h = h0; h < h1; ++h)
+    for (int h = from_head; h < to_head; ++h)
       *reinterpret_cast<Some<V>*>(to(h) + d) = *reinterpret_cast<const Some<V>*>(from(h) + d);
     return;
   }
   const int i0 = u * V;
   const int d1 = ADJACENT ? 2 * i0 : i0, d2 = ADJACENT ? 2 * i0 + V : i0 + a.half;
-  Some<V> x[HEADS][2];
-#pragma unroll
-  for (int e = 0; e < HEADS; ++e) {
-    const uint16_t* p = from(min(h0 + e, h1 - 1));
-    x[e][0] = *reinterpret_cast<const Some<V>*>(p + d1);
-    x[e][1] = *reinterpret_cast<const Some<V>*>(p + d2);
-  }
   float c[V], s[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -64,33 +59,42 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
     s[i] *= a.scale * a.sign;
     c[i] *= a.scale;
   }
+  for (int h0 = from_head; h0 < to_head; h0 += HEADS) {
+    Some<V> x[HEADS][2];
 #pragma unroll
-  for (int e = 0; e < HEADS; ++e) {
-    if (h0 + e >= h1) break;
-    Some<V> y[2];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      // Pair i: element i of either, or elements 2i and 2i + 1 of both as one.
-      const float x1 = ADJACENT ? (float)x[e][2 * i / V].v[2 * i % V] : (float)x[e][0].v[i];
-      const float x2 = ADJACENT ? (float)x[e][(2 * i + 1) / V].v[(2 * i + 1) % V] : (float)x[e][1].v[i];
-      const _Float16 y1 = (_Float16)fmaf(x1, c[i], -(x2 * s[i])), y2 = (_Float16)fmaf(x2, c[i], x1 * s[i]);
-      if (ADJACENT) {
-        y[2 * i / V].v[2 * i % V] = y1;
-        y[(2 * i + 1) / V].v[(2 * i + 1) % V] = y2;
-      } else {
-        y[0].v[i] = y1;
-        y[1].v[i] = y2;
-      }
+    for (int e = 0; e < HEADS; ++e) {
+      const uint16_t* p = from(min(h0 + e, to_head - 1));
+      x[e][0] = *reinterpret_cast<const Some<V>*>(p + d1);
+      x[e][1] = *reinterpret_cast<const Some<V>*>(p + d2);
     }
-    uint16_t* p = to(h0 + e);
-    *reinterpret_cast<Some<V>*>(p + d1) = y[0];
-    *reinterpret_cast<Some<V>*>(p + d2) = y[1];
+#pragma unroll
+    for (int e = 0; e < HEADS; ++e) {
+      if (h0 + e >= to_head) break;
+      Some<V> y[2];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        // Pair i: element i of either, or elements 2i and 2i + 1 of both as one.
+        const float x1 = ADJACENT ? (float)x[e][2 * i / V].v[2 * i % V] : (float)x[e][0].v[i];
+        const float x2 = ADJACENT ? (float)x[e][(2 * i + 1) / V].v[(2 * i + 1) % V] : (float)x[e][1].v[i];
+        const _Float16 y1 = (_Float16)fmaf(x1, c[i], -(x2 * s[i])), y2 = (_Float16)fmaf(x2, c[i], x1 * s[i]);
+        if (ADJACENT) {
+          y[2 * i / V].v[2 * i % V] = y1;
+          y[(2 * i + 1) / V].v[(2 * i + 1) % V] = y2;
+        } else {
+          y[0].v[i] = y1;
+          y[1].v[i] = y2;
+        }
+      }
+      uint16_t* p = to(h0 + e);
+      *reinterpret_cast<Some<V>*>(p + d1) = y[0];
+      *reinterpret_cast<Some<V>*>(p + d2) = y[1];
+    }
   }
 }
 
 template <int V, int HEADS>
 hipError_t start(const RopeArgs& a, bool adjacent, hipStream_t s) {
-  const dim3 grid((a.n_tokens + a.tokens - 1) / a.tokens, (a.heads + HEADS - 1) / HEADS, (a.units + 255) / 256);
+  const dim3 grid((a.n_tokens + a.tokens - 1) / a.tokens, (a.heads + a.per - 1) / a.per, (a.units + 255) / 256);
   if (adjacent)
     rope_kernel<V, HEADS, true><<<grid, 256, 0, s>>>(a);
   else
@@ -129,6 +133,11 @@ hipError_t launch_rope(const tq_rope_call& c, hipStream_t s) {
   a.turning = a.half / V;
   a.units = a.turning + rest / V;
   a.tokens = a.units <= 256 ? 256 / a.units : 1;
+  // Heads of a workgroup: four where there are few tokens, as many as leave two
+  // workgroups a CU, up to 20, where there are many (32 + 8 heads of 128: one
+  // token 5.2 us, with 20 heads a workgroup 9.2; 8191 tokens 35 us, with 4 41).
+  const int64_t fours = (int64_t)((a.n_tokens + a.tokens - 1) / a.tokens) * ((a.heads + 3) / 4);
+  a.per = 4 * (int)(fours < 1024 ? 1 : fours < 2560 ? fours / 512 : 5);
   const bool adjacent = c.flags & TQ_ROPE_ADJACENT;
   if (V == 8) return start<8, 4>(a, adjacent, s);
   if (V == 4) return start<4, 4>(a, adjacent, s);

@@ -1036,7 +1036,7 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
         scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail)
     qr = _kv_rows(q, None, cache.head_dim, "q")
     if o is None:
-        o = torch.empty((T, n_heads, D), dtype=torch.float32, device=q.device) if out_f32 else q.new_empty(q.shape)
+        o = torch.empty((T, n_heads, D), dtype=torch.float32, device=q.device) if out_f32 else _new_like(q)
     else:
         _out_buffer(o, (T, n_heads, D), torch.float32 if out_f32 else torch.float16, "o")
     if lse is None:
@@ -1087,6 +1087,12 @@ def _heads(t, shape, name):
     return t.data_ptr(), ts, hs
 
 
+def _new_like(t):
+    """A new tensor of t's shape and type, its elements adjacent."""
+    # (empty_like takes 1.1 us, new_empty of a shape 1.7.)
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, scale=1.0, q_out=None, k_out=None,
             stream=None):
     """Rotary positions of q [T, heads, D] and k [T, kv_heads, D] (None: q
@@ -1116,7 +1122,7 @@ def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, sca
         raise ValueError("several axes need axis")
     qr = _heads(q, shape, "q")
     if q_out is None:
-        q_out = q.new_empty(shape)
+        q_out = _new_like(q)
         qo = (q_out.data_ptr(), n_heads * D, D)
     else:
         qo = _heads(q_out, shape, "q_out")
@@ -1126,7 +1132,7 @@ def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, sca
         kv_heads = k.shape[1] if k.dim() == 3 else 0
         kr = _heads(k, (T, kv_heads, D), "k")
         if k_out is None:
-            k_out = k.new_empty(k.shape)
+            k_out = _new_like(k)
             ko = (k_out.data_ptr(), kv_heads * D, D)
         else:
             ko = _heads(k_out, k.shape, "k_out")
@@ -1174,12 +1180,12 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
         if ids.dim() not in (1, 2) or ids.shape[0] != T:
             raise ValueError("ids must be int32 [T] or [T, m]")
         m = 1 if ids.dim() == 1 else ids.shape[1]
-        logp = ids.new_empty(ids.shape, dtype=torch.float32)
+        logp = torch.empty_like(ids, dtype=torch.float32)
     if want_entropy:
         entropy = logits.new_empty(T, dtype=torch.float32)
     if top > 0:
-        top_ids = logits.new_empty((T, top), dtype=torch.int32)
         top_logp = logits.new_empty((T, top), dtype=torch.float32)
+        top_ids = torch.empty_like(top_logp, dtype=torch.int32)
     members = [T, V, m, top, LOGITS_FP32 if logits.dtype is torch.float32 else LOGITS_FP16, scale, logits.data_ptr(),
                ld if T > 1 else V, *[0 if t is None else t.data_ptr() for t in (ids, logp, entropy, top_ids, top_logp)],
                _i32(d_err, 1, "d_err") or 0, 0, 0]

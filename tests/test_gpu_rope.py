@@ -55,6 +55,21 @@ def test_shapes(D, rot, adjacent, T, hq, hkv):
     check(a, q, pos, f, adjacent=adjacent)
 
 
+@pytest.mark.parametrize("T,hq,hkv,D,rot", [(27000, 30, 9, 16, 16), (65537, 30, 9, 16, 16), (20011, 17, 6, 6, 2),
+                                            (700, 5, 2, 1023, 510)])
+def test_many_tokens(T, hq, hkv, D, rot):
+    """Enough of them that one workgroup takes more heads than it loads at once."""
+    q, k = _x((T, hq, D), D), _x((T, hkv, D), rot)
+    f = _freq(rot // 2)
+    pos = np.random.default_rng(T).integers(0, 100000, T).astype(np.int32)
+    a, b = tq.tq_rope(up(q), up(k), up(pos), up(f))
+    check(a, q, pos, f)
+    check(b, k, pos, f)
+    c = up(k)
+    tq.tq_rope(c, None, up(pos), up(f), q_out=c)
+    assert torch.equal(c, b)
+
+
 @pytest.mark.parametrize("axes", [2, 3, 8])
 @pytest.mark.parametrize("inverse", [False, True])
 def test_axes(axes, inverse):
