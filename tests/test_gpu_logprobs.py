@@ -101,6 +101,19 @@ def test_masks_ties_and_scales(f32, scale):
 
 
 @pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("scale", [1e-6, 333.0, 1e5, 1e9, 1e18])
+def test_small_and_large_scales(f32, scale):
+    """A small or a large temperature, up to one that leaves the largest logits alone."""
+    x = logits(5, 9000, 8, f32, 0.1)
+    x[1] += 100
+    x[2] *= 1e-3
+    x[3, 77] = x[3, 8888] = 60000                           # two of them, alike
+    x[4] = -np.abs(x[4]) - 5000
+    ids = np.tile([[77, 8888, 5]], (5, 1))
+    check(x, run(x, ids, top=9, scale=scale), ids, 9, scale)
+
+
+@pytest.mark.parametrize("f32", [False, True])
 def test_nothing_possible_and_special_values(f32):
     x = logits(9, 9000, 4, f32)
     low = np.finfo(x.dtype).min
