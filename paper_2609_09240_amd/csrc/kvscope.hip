@@ -2,7 +2,10 @@
 // rows that share the pages of a prefix (gfx950).
 //
 // Sinks: the records of a tile are those of its window and, in front of them,
-// the first ones of the slot; masks in the records where they end.
+// the first ones of the slot; masks in the records where they end.  The host
+// decides the parts and the waves (8 of them to a tile where the chip is not full:
+// 32 rows of 8 heads behind a window of 1024 and 4 sinks 15.6 us, where the launch
+// for rows without sinks takes 23.6 behind the same window).
 //
 // Shared prefixes.  The softmax over all tokens of a row is joined from those over
 // any parts of them: with m the largest logit of a part, l = sum exp(s - m) and
@@ -10,7 +13,14 @@
 //     o = sum_parts exp(m - M) y / sum_parts exp(m - M) l,   M = max of the m.
 // One launch takes the queries of all rows of a group as the rows of its tiles
 // over the shared records, and every row over what it has behind them; a second
-// one joins.
+// one joins.  (Unpacking a record once into LDS for 128 or 256 stacked rows, as two
+// fp16 halves of every value, took 1.3 to 1.8 times as long up to 8192 shared
+// tokens, and as long with its additional launch at 64 rows x 32768.)
+//
+// What bounds it (8 heads of 128, groups of 64): 64 rows x 4 heads over 32768
+// shared tokens 108 us, of which vector instructions, 383 a record and tile, are 83
+// and matrix instructions 21; 16 rows over 8000 19.7: four to six records a wave
+// behind a chain of loads.  The join 4 to 6.
 
 #include "decode_internal.h"
 #include "kvattn_kernel.h"
@@ -197,7 +207,9 @@ __global__ void __launch_bounds__(256) shared_prefix_kernel(KvDev c, const int32
       if (!same) atomicMin(&first, p);
     }
     __syncthreads();
-    if (first != INT32_MAX) break;
+    const int found = first;
+    __syncthreads();   // all have looked before the next pages can change it
+    if (found != INT32_MAX) break;
   }
   const int tokens = n > 0 ? (int)min((int64_t)min(first, n) << c.page_shift, (int64_t)least) : 0;
   for (int r = r0 + tid; r < r1; r += 256) prefix[r] = slot_of(r) >= 0 ? tokens : 0;

@@ -271,6 +271,23 @@ def test_prefixes_of_many_rows_and_pages():
     assert got.tolist() == decode.shared_prefix(pages.tolist(), lens.tolist(), 32, 5000, list(range(40)), [3, 30])
 
 
+@pytest.mark.parametrize("rows_", [2, 9, 40])
+def test_prefixes_that_end_in_several_places(rows_):
+    """Behind the first pages looked at, every row names another one somewhere: the
+    first of those places counts, whoever finds one first."""
+    r = np.random.default_rng(rows_)
+    c = tq.KVCache.empty(1, 5000, rows_, 1500, 1, 64, 32, 64)
+    for _ in range(20):
+        pages = np.tile(r.permutation(5000)[:1500].astype(np.int32), (rows_, 1))
+        for s in range(1, rows_):
+            at = int(r.integers(256, 1500))
+            pages[s, at] = 4999 - pages[s, at]
+        c.pages.copy_(torch.from_numpy(pages))
+        c.lens.fill_(1500 * 32)
+        got = tq.tq_kv_shared_prefix(c)
+        assert got.tolist() == [32 * int((pages != pages[0]).any(0).argmax())] * rows_
+
+
 def test_refusals():
     m = Branches([100], [0, 0], [3, 3], 1, 64, 64, 32)
     q = torch.zeros((2, 2, 64), dtype=torch.float16, device="cuda")
