@@ -175,7 +175,7 @@ struct MoreArgs : Args {
   int32_t parts;           // of a row's own tokens
   int32_t stack_parts;     // of shared tokens; those parts come first
   int32_t stack_blocks;    // workgroups of kv_attn_kernel for those, before the others
-  int32_t stack_tiles, n_groups;
+  int32_t n_groups;
   int32_t sinks;
 };
 
@@ -222,9 +222,34 @@ __device__ inline int shared_of(const MoreArgs& a, int row) {
   return (int)min(max((int64_t)as_table(a.prefix)[row], (int64_t)0), most) & ~31;
 }
 
-// Tile qt of group g, whose pages are those of its first row that shares any; false
-// where there is none.
-__device__ inline bool stack_of(const MoreArgs& a, int g, int qt, Tile* t) {
+// The first token of group g, or the token behind the last one.
+__device__ inline int stack_start(const MoreArgs& a, int g) {
+  const int row = min(max(a.cu_rows[g], 0), a.n_rows);
+  return min(max(a.cu ? a.cu[row] : row, 0), a.n_tokens);
+}
+
+// Tile j of those of all groups in a line; false where there is none.  The pages
+// are those of its group's first row that shares any.
+__device__ inline bool stack_of(const MoreArgs& a, int j, Tile* t) {
+  // Groups are counted by the lanes, `per` of them each, then those of the lane
+  // that has the tile.  (As many tiles for every group as all of them have took
+  // 166 us for 64 groups of 8 rows over 2048 tokens, this 100; a tile that none has
+  // behind every group's costs half of the chip where groups have one tile.)
+  int g = 0, qt = j;
+  for (int n = a.n_groups; n > 1;) {
+    const int per = (n + 63) / 64, at = ((int)threadIdx.x & 63) * per;
+    int sum = 0, from = at < n ? stack_start(a, g + at) : 0;
+    for (int e = at; e < min(at + per, n); ++e) {
+      const int to = stack_start(a, g + e + 1);
+      sum += (max(to - from, 0) * a.share + 15) >> 4;
+      from = to;
+    }
+    const int before = wave_scan(sum) - sum;
+    const int k = max(__popcll(__builtin_amdgcn_ballot_w64(at < n && before <= qt)), 1) - 1;
+    qt -= __builtin_amdgcn_readlane(before, k);
+    g += k * per;
+    n = min(per, n - k * per);
+  }
   const int r0 = a.cu_rows ? as_table(a.cu_rows)[g] : 0, r1 = a.cu_rows ? as_table(a.cu_rows)[g + 1] : a.n_rows;
   if (r0 < 0 || r1 > a.n_rows) return false;
   int lead = r0;
@@ -449,14 +474,13 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
   bool all_of_it = true, stacked = false;
   const int slot = 2 * blockIdx.x + (share.unit != first_unit);
   if constexpr (MODE != kPlain) {
-    // Heads beside each other, then parts, rows, tiles.
+    // Heads beside each other, then parts, rows (stacked: tiles of a group), tiles.
     int id = blockIdx.x;
     stacked = MODE == kShared && id < a.stack_blocks;
     if (MODE == kShared && !stacked) id -= a.stack_blocks;
-    const int parts = stacked ? a.stack_parts : a.parts, n = stacked ? a.n_groups : a.n_rows;
-    const int i = id / a.H, j = i / parts, qt = j / n;
+    const int parts = stacked ? a.stack_parts : a.parts, i = id / a.H, j = i / parts, qt = j / a.n_rows;
     part = i - j * parts;
-    if (!(stacked ? stack_of(a, j - qt * n, qt, &t) : tile_of<MODE>(a, j - qt * n, qt, &t))) return;
+    if (!(stacked ? stack_of(a, j, &t) : tile_of<MODE>(a, j - qt * a.n_rows, qt, &t))) return;
     t.h = id - i * a.H;
     const int64_t all = t.rec1 - t.rec0;
     rec0 = t.rec0 + (int)(all * part / parts);

@@ -32,7 +32,7 @@ struct ScopePlan {
   bool plain, sinks;    // neither: shared
   int waves;            // of a workgroup of kv_attn_kernel
   int tiles, parts;     // of a row, 16 query rows each; of its own tokens
-  int stack_tiles, stack_parts;   // of a group
+  int stack_tiles, stack_parts;   // of all groups; of a group's shared tokens
   size_t bytes;         // workspace behind the counts
 };
 
@@ -42,30 +42,29 @@ struct Work {
 };
 
 // What a launch of workgroups of `waves` waves takes (us), where `a` and `b` are cut
-// into parts: 2.5 for what starts and ends a workgroup, 1 for a record of a wave
-// alone on its SIMD, 0.6 of a SIMD's time for each where several are.
+// into parts.  A CU has its share of the workgroups of `a`, a whole number, and of
+// those of `b`.  A record takes a wave alone on its SIMD 1, two waves 1.6 and three 2.3;
+// 2.5 start and end a round of workgroups, 0.12 joins a part.  (64 rows of 4 heads over
+// 32768 shared tokens, of which 128 tiles and heads are cut into 1, 2, 3, 4, 6, 8 parts:
+// 264, 140, 150, 117, 113, 113 us; 16 rows over 8000, 32 of them into 5, 6, 7, 8, 10, 12,
+// 15, 18: 24.8, 22.9, 21.1, 20.3, 23.6, 22.2, 20.9, 22.8.)
 double cost(const KvDev& c, int waves, Work a, int parts_a, Work b, int parts_b) {
   const int lds = waves * 16 * (c.D + 6) * 4, by_lds = 160 * 1024 / lds, by_waves = 4 * waves_of(c.D, c.G) / waves;
-  const int64_t slots = (int64_t)kCus * (by_lds < by_waves ? by_lds : by_waves), n = a.ids * parts_a + b.ids * parts_b;
-  const double resident = (double)(n < slots ? n : slots), load = resident * waves / (4 * kCus);
-  const double each = 0.6 * load > 1.0 ? 0.6 * load : 1.0;
-  const double recs_a = a.ids > 0 ? (double)(a.recs + parts_a * waves - 1) / (parts_a * waves) : 0.0;
-  const double recs_b = b.ids > 0 ? (double)(b.recs + parts_b * waves - 1) / (parts_b * waves) : 0.0;
-  // One round: the longest workgroup; several: what there is, evenly.
-  double recs = recs_a > recs_b ? recs_a : recs_b;
-  const int64_t rounds = (n + slots - 1) / slots;
-  if (rounds > 1) {
-    const double even = (recs_a * a.ids * parts_a + recs_b * b.ids * parts_b) / slots;
-    recs = recs > even ? recs : even;
-  }
-  return 2.5 * rounds + recs * each;
+  const int64_t slots = (int64_t)kCus * (by_lds < by_waves ? by_lds : by_waves);
+  const int64_t n_a = a.ids * parts_a, n_b = b.ids * parts_b, rounds = (n_a + n_b + slots - 1) / slots;
+  const double recs_a = a.ids > 0 ? (double)((a.recs + parts_a * waves - 1) / (parts_a * waves)) : 0.0;
+  const double recs_b = b.ids > 0 ? (double)((b.recs + parts_b * waves - 1) / (parts_b * waves)) : 0.0;
+  const double longest = recs_a > recs_b ? recs_a : recs_b;
+  const double of_simd = waves / 4.0 * ((double)((n_a + kCus - 1) / kCus) * recs_a + (double)n_b / kCus * recs_b);
+  const double busy = 0.73 * of_simd + 0.13 * longest;
+  return 2.5 * rounds + (busy > longest ? busy : longest) + 0.12 * (parts_a + parts_b);
 }
 
 // The best parts of `a` beside `b`, in workgroups of `waves` waves; `join`: what
-// joining parts takes.  A part is a record a wave at least.
+// another launch that joins parts takes.  A part is a record a wave at least.
 double split(const KvDev& c, int waves, Work a, Work b, int parts_b, double join, int* parts) {
   double best = 1e30;
-  for (int n = 1; n <= kMaxParts && (n == 1 || a.recs >= (int64_t)waves * n); n += n < 4 ? 1 : n / 4) {
+  for (int n = 1; n <= kMaxParts && (n == 1 || a.recs >= (int64_t)waves * n); n += n < 16 ? 1 : n / 8) {
     const double t = cost(c, waves, a, n, b, parts_b) + (n > 1 ? join : 0.0);
     if (t < best) {
       best = t;
@@ -92,8 +91,8 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
     const int64_t stacked = (int64_t)a.n_tokens * share;
     const int64_t prefix = (sc.max_prefix > 0 ? sc.max_prefix : hint) / 32;
     const int64_t tail = (sc.max_tail > 0 ? (int64_t)sc.max_tail + 31 : hint) / 32 + 1;
-    const int64_t stack_tiles = (stacked + 15) / 16, stack_ids = (stack_tiles + sc.n_groups) * c.H;
-    if (stack_tiles <= 65535 && ids <= kMostOfTwo && stack_tiles * sc.n_groups * c.H <= kMostOfTwo) {
+    const int64_t stack_tiles = (stacked + 15) / 16 + sc.n_groups - 1, stack_ids = stack_tiles * c.H;
+    if (ids <= kMostOfTwo && stack_ids <= kMostOfTwo) {
       p->stack_tiles = (int)stack_tiles;
       const Work stack{stack_ids, prefix}, rest{ids, tail}, none{0, 0};
       split(c, 4, rest, none, 1, 0.0, &p->parts);
@@ -238,7 +237,6 @@ hipError_t launch_kv_attention_scope(const KvDev& c, int layer, const AttnCall& 
   a.pre_part = (int64_t)call.n_tokens * call.n_heads * (c.D + 4);
   a.parts = p.parts;
   a.stack_parts = p.stack_parts;
-  a.stack_tiles = p.stack_tiles;
   a.n_groups = sc.n_groups;
   a.stack_blocks = 0;
   a.sinks = sc.sinks;
@@ -247,7 +245,7 @@ hipError_t launch_kv_attention_scope(const KvDev& c, int layer, const AttnCall& 
     e = start<kSinks>(c, a, p, s);
     return e == hipSuccess && p.parts > 1 ? start_join<kSinks>(c, a, s) : e;
   }
-  a.stack_blocks = c.H * p.stack_parts * sc.n_groups * p.stack_tiles;
+  a.stack_blocks = c.H * p.stack_parts * p.stack_tiles;
   e = start<kShared>(c, a, p, s);
   return e == hipSuccess ? start_join<kShared>(c, a, s) : e;
 }

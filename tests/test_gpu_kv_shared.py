@@ -271,6 +271,28 @@ def test_prefixes_of_many_rows_and_pages():
     assert got.tolist() == decode.shared_prefix(pages.tolist(), lens.tolist(), 32, 5000, list(range(40)), [3, 30])
 
 
+@pytest.mark.parametrize("n_groups,most", [(64, 30), (65, 9), (130, 5), (4300, 3)])
+def test_many_groups(n_groups, most):
+    """More groups than a wave has lanes, some of them empty, rows without queries and
+    with several; rows of one slot share its first tokens."""
+    m = Branches([40, 100, 64], [], [], 1, 64, 32, 32)
+    r = np.random.default_rng(n_groups)
+    sizes = r.integers(0, most + 1, n_groups)
+    sizes[[0, -1]] = 2
+    groups = [0, *np.cumsum(sizes).tolist()]
+    seqs = np.repeat(r.integers(0, 3, n_groups), sizes).tolist()
+    nq = r.integers(0, 4, len(seqs)).tolist()
+    q = rows((sum(nq), 3, 64), 8)
+    prefix = np.repeat(np.where(sizes > 1, [[32], [96]], 0)[r.integers(0, 2, n_groups), np.arange(n_groups)], sizes)
+    prefix = np.minimum(prefix, np.array([40, 100, 64])[seqs])
+    o, lse = run(m, q, nq, seqs, groups, prefix=i32(*prefix.tolist()), **FEW)
+    assert bool(torch.isfinite(o).all())
+    some = sorted(set(r.integers(0, len(seqs), 60).tolist()) | {0, len(seqs) - 1})
+    starts = np.concatenate([[0], np.cumsum(nq)])
+    at = np.concatenate([np.arange(starts[i], starts[i + 1]) for i in some]).astype(np.int64)
+    check(m, q[at], [nq[i] for i in some], o[at], lse[at], seqs=[seqs[i] for i in some])
+
+
 @pytest.mark.parametrize("rows_", [2, 9, 40])
 def test_prefixes_that_end_in_several_places(rows_):
     """Behind the first pages looked at, every row names another one somewhere: the
