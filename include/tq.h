@@ -655,7 +655,8 @@ tq_status tq_kv_shared_prefix(const tq_kv_cache* cache, const int32_t* seqs, con
  * output.  Angles are reduced in 64 bits, at any position; products and sums
  * are fp32, rounded once to fp16.
  * In place (an output with the data and the strides of its input) or into
- * memory that does not overlap any input. */
+ * memory that does not overlap any input; outputs overlap neither themselves
+ * nor each other (strides of 0 are refused). */
 #define TQ_ROPE_ADJACENT 1
 #define TQ_ROPE_INVERSE 2
 #define TQ_ROPE_MAX_DIM 1024

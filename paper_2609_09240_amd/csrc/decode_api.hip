@@ -36,6 +36,11 @@ tq_status check_logprobs(const tq_logprobs_call* c) {
   return TQ_OK;
 }
 
+// Rows that do not lie on each other.
+bool apart(const tq_out_rows& o, int32_t n_tokens, int32_t n_heads) {
+  return (n_tokens == 1 || o.token_stride != 0) && (n_heads == 1 || o.head_stride != 0);
+}
+
 bool same_rows(const tq_kv_rows& r, const tq_out_rows& o) {
   return r.data == o.data && r.token_stride == o.token_stride && r.head_stride == o.head_stride;
 }
@@ -105,6 +110,8 @@ tq_status tq_rope(const tq_rope_call* c, void* stream) {
   if (misaligned(c->positions, 4) || misaligned(c->freq, 4) || misaligned(c->q.data, 2) || misaligned(c->q_out.data, 2) ||
       misaligned(c->k.data, 2) || misaligned(c->k_out.data, 2))
     return TQ_ERR_ALIGN;
+  if (!apart(c->q_out, c->n_tokens, c->n_heads) || (c->n_kv_heads > 0 && !apart(c->k_out, c->n_tokens, c->n_kv_heads)))
+    return TQ_ERR_SHAPE;
   // An output that starts where its input does is the input.
   if ((c->q.data == c->q_out.data && !same_rows(c->q, c->q_out)) ||
       (c->n_kv_heads > 0 && c->k.data == c->k_out.data && !same_rows(c->k, c->k_out)))

@@ -998,6 +998,7 @@ def tq_kv_shared_prefix(cache, groups=None, seqs=None, prefix=None, stream=None)
     of them without.  Once after the page table changed, for all layers."""
     n = _n_rows(cache, seqs, None)
     n_groups = 1 if groups is None else groups.numel() - 1
+    _here(cache.lens)
     if prefix is None:
         prefix = torch.empty(n, dtype=torch.int32, device=cache.lens.device)
     _check(lib().tq_kv_shared_prefix(cache._ref, _i32(seqs, n, "seqs"), _i32(groups, n_groups + 1, "groups"), n_groups, n,
@@ -1033,6 +1034,7 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
     _fits(layer | max_q | max_len | window | sinks | max_prefix | max_tail)
     scope = None
     if sinks or prefix is not None or groups is not None:
+        _here(q)
         scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail)
     qr = _kv_rows(q, None, cache.head_dim, "q")
     if o is None:
@@ -1087,6 +1089,13 @@ def _heads(t, shape, name):
     return t.data_ptr(), ts, hs
 
 
+def _here(t):
+    """Refuses a tensor of another device than the current one, whose stream a
+    call goes to."""
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError("the tensors must be on the current device")
+
+
 def _new_like(t):
     """A new tensor of t's shape and type, its elements adjacent."""
     # (empty_like takes 1.1 us, new_empty of a shape 1.7.)
@@ -1136,6 +1145,7 @@ def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, sca
             ko = (k_out.data_ptr(), kv_heads * D, D)
         else:
             ko = _heads(k_out, k.shape, "k_out")
+    _here(q)
     call = _ROPE_CALL.pack(T, n_heads, kv_heads, D, 2 * n, axes,
                            (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0), scale,
                            positions.data_ptr(), 0 if axes == 1 else positions.stride(0), freq.data_ptr(),
@@ -1173,6 +1183,7 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
     if one != 1 and V != 1:
         raise ValueError("logits must have adjacent elements in a row")
     _fits(T | V | top)
+    _here(logits)
     logp = entropy = top_ids = top_logp = None
     m = 0
     if ids is not None:

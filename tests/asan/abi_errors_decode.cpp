@@ -231,6 +231,8 @@ int main() {
     c = rope(); c.freq = fake<const float>(2); expect("rope: freq align", run(), TQ_ERR_ALIGN);
     c = rope(); c.q.data = fake<const uint16_t>(1); expect("rope: q align", run(), TQ_ERR_ALIGN);
     c = rope(); c.k_out.data = fake<uint16_t>(1); expect("rope: k_out align", run(), TQ_ERR_ALIGN);
+    c = rope(); c.q_out.token_stride = 0; expect("rope: tokens on each other", run(), TQ_ERR_SHAPE);
+    c = rope(); c.k_out.head_stride = 0; expect("rope: heads on each other", run(), TQ_ERR_SHAPE);
     c = rope(); c.q_out.data = fake<uint16_t>(0x10000); c.q_out.token_stride = 513;
     expect("rope: in place with other strides", run(), TQ_ERR_SHAPE);
     c = rope(); c.k_out.data = fake<uint16_t>(0x20000); c.k_out.head_stride = 130;

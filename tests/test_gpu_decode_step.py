@@ -148,3 +148,19 @@ def test_two_captured_steps_give_what_the_calls_give():
         tq.tq_kv_attention(c, 0, s.parts(0)[0], seqs=s.seqs, prefix=s.prefix, max_prefix=1 << 20)
     for a, b in zip(c._buffers()[1:], end[1:]):
         assert torch.equal(a, b)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    s = Step(5)
+    s.fill(1)
+    q = s.parts(0)[0]
+    calls = (lambda: tq.tq_rope(q, None, s.pos[0].zero_(), s.freq), lambda: tq.tq_logprobs(s.freq.view(1, 64), top=1),
+             lambda: tq.tq_kv_shared_prefix(s.m.cache, seqs=s.seqs),
+             lambda: tq.tq_kv_attention(s.m.cache, 0, q, seqs=s.seqs, prefix=s.prefix),
+             lambda: tq.tq_kv_attention(s.m.cache, 0, q, seqs=s.seqs, window=9, sinks=1))
+    for call in calls:
+        call()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()

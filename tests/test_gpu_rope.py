@@ -208,3 +208,5 @@ def test_refusals():
     other = wide.as_strided((4, 2, 64), (256, 128, 1))
     with pytest.raises(tq.TqError):                     # starts where the input does, with other strides
         tq.tq_rope(view, None, pos, f, q_out=other)
+    with pytest.raises(tq.TqError):                     # a row that all tokens are written to
+        tq.tq_rope(q, None, pos, f, q_out=torch.empty_like(q[:1]).expand(4, 2, 64))
