@@ -141,8 +141,8 @@ __device__ inline float log2_of(float x) { return (float)((int)(__builtin_bit_ca
 // of a slot beside a window.  kShared: groups of rows over the tokens that they share
 // (stacked: the queries of all of a group's rows as the rows of its tiles), and
 // rows over what is behind those.  (A chunk of 2 x 700 queries over up to 5000, 14
-// heads of 64 on 2, groups of 32, window 777 and 37 sinks: 31 us, 358 vector
-// instructions a record and tile, 63 % of the vector slots.)
+// heads of 64 on 2, groups of 32, window 777 and 37 sinks: 32 us, 359 vector
+// instructions a record and tile, 61 % of the vector slots.)
 enum { kPlain, kSinks, kShared };
 
 struct Args {

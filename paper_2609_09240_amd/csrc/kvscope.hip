@@ -4,7 +4,7 @@
 // Sinks: the records of a tile are those of its window and, in front of them,
 // the first ones of the slot; masks in the records where they end.  The host
 // decides the parts and the waves (8 of them to a tile where the chip is not full:
-// 32 rows of 8 heads behind a window of 1024 and 4 sinks 15.6 us, where the launch
+// 32 rows of 8 heads behind a window of 1024 and 4 sinks 15.4 us, where the launch
 // for rows without sinks takes 23.6 behind the same window).
 //
 // Shared prefixes.  The softmax over all tokens of a row is joined from those over
@@ -18,9 +18,9 @@
 // tokens, and as long with its additional launch at 64 rows x 32768.)
 //
 // What bounds it (8 heads of 128, groups of 64): 64 rows x 4 heads over 32768
-// shared tokens 108 us, of which vector instructions, 383 a record and tile, are 83
-// and matrix instructions 21; 16 rows over 8000 19.7: four to six records a wave
-// behind a chain of loads.  The join 4 to 6.
+// shared tokens 111 us, of which vector instructions, 391 a record and tile, are 85
+// and matrix instructions 21; 16 rows over 8000 17.4: eight records a wave behind a
+// chain of loads.  The join 4 to 7.
 
 #include "decode_internal.h"
 #include "kvattn_kernel.h"

@@ -16,9 +16,10 @@
 // workgroup of a row to leave its part joins them in their order.
 //
 // Bound by memory where rows are many and long: 1500 rows of 49999 fp16 logits
-// (150 MB) with the most likely one 45.7 us, 3.3 TB/s; without 39.  Few rows: 64
-// of 131072 fp32 logits (34 MB) 21 us with the 20 most likely ones, 13 without;
-// 1 row of 5000 6.5: launch, two trips to memory, ranking, the join.
+// (150 MB) with the most likely one 47.6 us, 3.2 TB/s, of which vector instructions
+// are 32; without 39.  Few rows: 64 of 131072 fp32 logits (34 MB) 21 us with the 20
+// most likely ones, 13 without; 1 row of 5000 6.7: launch, two trips to memory,
+// ranking, the join.
 
 #include "decode_internal.h"
 
