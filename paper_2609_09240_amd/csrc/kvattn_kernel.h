@@ -1004,12 +1004,33 @@ __global__ void __launch_bounds__(256) kv_join_kernel(MoreArgs a) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAhead = 2 * kMaxParts / kGroups;
   __shared__ float4v ys[kGroups][kLanes];
   __shared__ float refs[kGroups], sums[kGroups];
-  const int b = blockIdx.y, heads = a.H * a.share;
+  const int heads = a.H * a.share;
+  int b, tok, head;
+  if constexpr (MODE == kShared) {
+    // A workgroup a token, which rows of many queries beside those of one ask for: its
+    // row is the last one that starts at or before it, 64 of them looked at at once.
+    b = tok = blockIdx.x;
+    head = blockIdx.y;
+    if (a.cu != nullptr) {
+      b = 0;
+      for (int n = a.n_rows; n > 1;) {
+        const int step = (n + 63) / 64, at = ((int)threadIdx.x & 63) * step;
+        const int start = at < n ? a.cu[b + at] : INT32_MAX;
+        const int k = max(__popcll(__builtin_amdgcn_ballot_w64(at < n && start <= tok)), 1) - 1;
+        n = min(step, n - k * step);
+        b += k * step;
+      }
+    }
+  } else {   // a row, and the token of it
+    b = blockIdx.y;
+    tok = (a.cu ? as_table(a.cu)[b] : b) + blockIdx.z;
+    head = blockIdx.x;
+  }
   const int64_t first = a.cu ? as_table(a.cu)[b] : b, end = a.cu ? as_table(a.cu)[b + 1] : (int64_t)b + 1;
   const int k1 = a.stack_parts + a.parts;
   const int k0 = MODE == kShared && shared_of(a, b) == 0 ? a.stack_parts : 0;
-  const int64_t at = (first + blockIdx.z) * heads + blockIdx.x;
-  if (first < 0 || first + blockIdx.z >= min(end, (int64_t)a.n_tokens)) return;
+  const int64_t at = (int64_t)tok * heads + head;
+  if (first < 0 || tok < first || tok >= min(min(end, (int64_t)a.n_tokens), first + a.max_q)) return;
   const int grp = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
   const float* p = a.pre + at * (D + 4);
   float4v v[kAhead], x[kAhead];
@@ -1059,7 +1080,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(MoreArgs a) {
 }
 
 // The split of a launch: `rows` rows of queries and heads at most in each of
-// `n` rows of the call (kStack: groups), `len` tokens as far as the caller knows.
+// `n` rows of the call, `len` tokens as far as the caller knows.
 // Everything here comes from the caller's sizes; the lengths themselves are on
 // the device.
 struct Plan {

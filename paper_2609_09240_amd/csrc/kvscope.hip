@@ -86,8 +86,7 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
   p->tiles = (int)tiles;
   p->bytes = 0;
   if (tiles > 65535 || ids > kMostIds) return false;
-  const bool joined = a.max_q <= 65535;   // a grid of rows and tokens
-  if (sc.n_groups > 0 && a.window == 0 && joined) {
+  if (sc.n_groups > 0 && a.window == 0 && a.n_tokens < 1 << 24) {   // (what a grid of tokens holds)
     const int64_t stacked = (int64_t)a.n_tokens * share;
     const int64_t prefix = (sc.max_prefix > 0 ? sc.max_prefix : hint) / 32;
     const int64_t tail = (sc.max_tail > 0 ? (int64_t)sc.max_tail + 31 : hint) / 32 + 1;
@@ -129,7 +128,7 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
     p->waves = 8;
     p->parts = n;
   }
-  if (!joined) p->parts = 1;
+  if (a.max_q > 65535) p->parts = 1;   // a grid of rows and tokens
   if (p->parts > 1) p->bytes = (size_t)p->parts * part_bytes;
   return true;
 }
@@ -149,7 +148,7 @@ hipError_t start(const KvDev& c, const MoreArgs& a, const ScopePlan& p, hipStrea
 
 template <int MODE>
 hipError_t start_join(const KvDev& c, const MoreArgs& a, hipStream_t s) {
-  const dim3 grid(a.H * a.share, a.n_rows, a.max_q);
+  const dim3 grid = MODE == kShared ? dim3(a.n_tokens, a.H * a.share) : dim3(a.H * a.share, a.n_rows, a.max_q);
   if (c.D == 64)
     kv_join_kernel<64, MODE><<<grid, 256, 0, s>>>(a);
   else if (c.D == 128)
