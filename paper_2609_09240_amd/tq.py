@@ -8,6 +8,7 @@ raises.
 """
 
 import ctypes
+import math
 import os
 import struct
 from dataclasses import dataclass
@@ -239,11 +240,10 @@ def lib():
             "tq_kv_copy_pages": ([cp, vp, vp, i32, vp, vp], ctypes.c_int),
             "tq_kv_append": ([cp, i32, vp, vp, vp, i32, i32, i32, rp, rp, vp, vp], ctypes.c_int),
             "tq_kv_read": ([cp, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp], ctypes.c_int),
-            "tq_kv_attention_workspace_bytes": ([cp, ctypes.POINTER(TqKvAttn)], ctypes.c_size_t),
-            "tq_kv_attention": ([cp, i32, ctypes.POINTER(TqKvAttn), vp], ctypes.c_int),
-            "tq_kv_attention_scope_workspace_bytes": ([cp, ctypes.POINTER(TqKvAttn), ctypes.POINTER(TqKvScope)],
-                                                      ctypes.c_size_t),
-            "tq_kv_attention_scope": ([cp, i32, ctypes.POINTER(TqKvAttn), ctypes.POINTER(TqKvScope), vp], ctypes.c_int),
+            "tq_kv_attention_workspace_bytes": ([cp, vp], ctypes.c_size_t),
+            "tq_kv_attention": ([cp, i32, vp, vp], ctypes.c_int),
+            "tq_kv_attention_scope_workspace_bytes": ([cp, vp, vp], ctypes.c_size_t),
+            "tq_kv_attention_scope": ([cp, i32, vp, vp, vp], ctypes.c_int),
             "tq_kv_shared_prefix": ([cp, vp, vp, i32, i32, vp, vp], ctypes.c_int),
             "tq_rope": ([vp, vp], ctypes.c_int),
             "tq_logprobs_workspace_bytes": ([vp], ctypes.c_size_t),
@@ -964,6 +964,30 @@ def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=N
     return k, v
 
 
+# tq_kv_attn, tq_kv_scope, tq_rope_call and tq_logprobs_call as bytes: building
+# a ctypes structure of as many members takes 2 us more.
+_ATTN_CALL = struct.Struct("@6ifiPPPqq3PN")
+_SCOPE_CALL = struct.Struct("@4iPP")
+_ROPE_CALL = struct.Struct("@7ifPqPP" + 4 * "Pqq")
+_LOGPROBS_CALL = struct.Struct("@5ifPq7PN")
+
+
+def _f32(x):
+    """A number as 32 bits; the library refuses infinities where one stands for what
+    does not fit them."""
+    return x if -3e38 < x < 3e38 else math.inf
+
+
+def _heads(t, shape, name):
+    """Address and strides of fp16 [T, heads, D] on the GPU, any strides but the last."""
+    if t.dtype is not torch.float16 or not t.is_cuda or t.shape != shape:
+        raise ValueError(f"{name} must be float16 {list(shape)} on the GPU")
+    ts, hs, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name} must have adjacent channels")
+    return t.data_ptr(), ts, hs
+
+
 def tq_kv_attention_workspace_bytes(cache, n_rows, n_heads, n_tokens=None, max_q=1, max_len=0, window=0, sinks=0,
                                     n_groups=0, max_prefix=0, max_tail=0):
     """Workspace of tq_kv_attention for n_rows rows of n_tokens queries together
@@ -972,12 +996,13 @@ def tq_kv_attention_workspace_bytes(cache, n_rows, n_heads, n_tokens=None, max_q
     T = n_rows * max_q if n_tokens is None else n_tokens
     _fits(n_rows | T | max_q | n_heads | max_len | window | sinks | n_groups | max_prefix | max_tail)
     # (Slots that are not read here: more rows than slots are allowed where rows name theirs.)
-    a = TqKvAttn(n_rows, T, max_q, n_heads, max_len, window, 1.0, OUT_FP16, cache.lens.data_ptr())
+    some = cache.lens.data_ptr()
+    a = _ATTN_CALL.pack(n_rows, T, max_q, n_heads, max_len, window, 1.0, OUT_FP16, some, *(0,) * 8)
     if not sinks and not n_groups:
         return int(lib().tq_kv_attention_workspace_bytes(cache._ref, a))
-    some = cache.lens.data_ptr()   # (rows and prefixes are not read here either)
+    # (Rows and prefixes are not read here either.)
     return int(lib().tq_kv_attention_scope_workspace_bytes(
-        cache._ref, a, TqKvScope(sinks, n_groups, max_prefix, max_tail, some, some)))
+        cache._ref, a, _SCOPE_CALL.pack(sinks, n_groups, max_prefix, max_tail, some, some)))
 
 
 def _scope(n, sinks, prefix, groups, max_prefix, max_tail):
@@ -985,10 +1010,10 @@ def _scope(n, sinks, prefix, groups, max_prefix, max_tail):
     if prefix is None:
         if groups is not None:
             raise ValueError("groups share what prefix says")
-        return TqKvScope(sinks, 0, 0, 0, None, None) if sinks else None
+        return _SCOPE_CALL.pack(sinks, 0, 0, 0, 0, 0) if sinks else None
     n_groups = 1 if groups is None else groups.numel() - 1
-    return TqKvScope(sinks, n_groups, max_prefix, max_tail, _i32(groups, n_groups + 1, "groups"),
-                     _i32(prefix, n, "prefix"))
+    return _SCOPE_CALL.pack(sinks, n_groups, max_prefix, max_tail, _i32(groups, n_groups + 1, "groups") or 0,
+                            _i32(prefix, n, "prefix"))
 
 
 def tq_kv_shared_prefix(cache, groups=None, seqs=None, prefix=None, stream=None):
@@ -1036,7 +1061,7 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
     if sinks or prefix is not None or groups is not None:
         _here(q)
         scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail)
-    qr = _kv_rows(q, None, cache.head_dim, "q")
+    qr = _heads(q, (T, n_heads, cache.head_dim), "q")
     if o is None:
         o = torch.empty((T, n_heads, D), dtype=torch.float32, device=q.device) if out_f32 else _new_like(q)
     else:
@@ -1046,9 +1071,10 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
             lse = torch.empty((T, n_heads), dtype=torch.float32, device=q.device)
     else:
         _out_buffer(lse, (T, n_heads), torch.float32, "lse")
-    a = TqKvAttn(n, T, max_q, n_heads, max_len, window, D ** -0.5 if scale is None else scale,
-                 OUT_FP32 if out_f32 else OUT_FP16, _i32(seqs, n, "seqs"), _i32(cu_q, n + 1, "cu_q"), qr,
-                 o.data_ptr(), None if lse is None else lse.data_ptr(), None, 0)
+    members = [n, T, max_q, n_heads, max_len, window, D ** -0.5 if scale is None else _f32(scale),
+               OUT_FP32 if out_f32 else OUT_FP16, _i32(seqs, n, "seqs") or 0, _i32(cu_q, n + 1, "cu_q") or 0, *qr,
+               o.data_ptr(), 0 if lse is None else lse.data_ptr(), 0, 0]
+    a = _ATTN_CALL.pack(*members)
     L = lib()
     if scope is None:
         need = L.tq_kv_attention_workspace_bytes(cache._ref, a)
@@ -1059,7 +1085,8 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
             workspace = cache._ws.get(need, stream)
         else:
             _cuda(workspace, torch.uint8, "workspace")
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        members[-2:] = workspace.data_ptr(), workspace.numel()
+        a = _ATTN_CALL.pack(*members)
     if scope is None:
         _check(L.tq_kv_attention(cache._ref, layer, a, _stream(stream)), "tq_kv_attention")
     else:
@@ -1072,22 +1099,6 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
 # --------------------------------------------------------------------------
 # Rotary positions and log probabilities.
 # --------------------------------------------------------------------------
-
-# tq_rope_call and tq_logprobs_call as bytes: building a ctypes structure of as
-# many members takes 2 us more.
-_ROPE_CALL = struct.Struct("@7ifPqPP" + 4 * "Pqq")
-_LOGPROBS_CALL = struct.Struct("@5ifPq7PN")
-
-
-def _heads(t, shape, name):
-    """Address and strides of fp16 [T, heads, D] on the GPU, any strides but the last."""
-    if t.dtype is not torch.float16 or not t.is_cuda or t.shape != shape:
-        raise ValueError(f"{name} must be float16 {list(shape)} on the GPU")
-    ts, hs, one = t.stride()
-    if one != 1:
-        raise ValueError(f"{name} must have adjacent channels")
-    return t.data_ptr(), ts, hs
-
 
 def _here(t):
     """Refuses a tensor of another device than the current one, whose stream a
@@ -1147,7 +1158,7 @@ def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, sca
             ko = _heads(k_out, k.shape, "k_out")
     _here(q)
     call = _ROPE_CALL.pack(T, n_heads, kv_heads, D, 2 * n, axes,
-                           (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0), scale,
+                           (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0), _f32(scale),
                            positions.data_ptr(), 0 if axes == 1 else positions.stride(0), freq.data_ptr(),
                            0 if axis is None else axis.data_ptr(), *qr, *kr, *qo, *ko)
     _check(lib().tq_rope(call, _stream(stream)), "tq_rope")
@@ -1197,8 +1208,9 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
     if top > 0:
         top_logp = logits.new_empty((T, top), dtype=torch.float32)
         top_ids = torch.empty_like(top_logp, dtype=torch.int32)
-    members = [T, V, m, top, LOGITS_FP32 if logits.dtype is torch.float32 else LOGITS_FP16, scale, logits.data_ptr(),
-               ld if T > 1 else V, *[0 if t is None else t.data_ptr() for t in (ids, logp, entropy, top_ids, top_logp)],
+    members = [T, V, m, top, LOGITS_FP32 if logits.dtype is torch.float32 else LOGITS_FP16, _f32(scale),
+               logits.data_ptr(), ld if T > 1 else V,
+               *[0 if t is None else t.data_ptr() for t in (ids, logp, entropy, top_ids, top_logp)],
                _i32(d_err, 1, "d_err") or 0, 0, 0]
     L = lib()
     call = _LOGPROBS_CALL.pack(*members)

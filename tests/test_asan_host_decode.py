@@ -66,7 +66,8 @@ def test_structs_match_the_header(tmp_path, name, mirror):
 
 
 def test_packed_calls_have_the_layout_of_their_structs():
-    for packed, mirror in ((tq._ROPE_CALL, tq.TqRopeCall), (tq._LOGPROBS_CALL, tq.TqLogprobsCall)):
+    for packed, mirror in ((tq._ROPE_CALL, tq.TqRopeCall), (tq._LOGPROBS_CALL, tq.TqLogprobsCall),
+                           (tq._ATTN_CALL, tq.TqKvAttn), (tq._SCOPE_CALL, tq.TqKvScope)):
         assert packed.size == ctypes.sizeof(mirror)
     # every member its own number, through the struct's names
     n = iter(range(1, 100))
@@ -82,6 +83,14 @@ def test_packed_calls_have_the_layout_of_their_structs():
     assert (call.n_rows, call.n_vocab, call.n_ids, call.n_top, call.flags, call.scale) == (1, 2, 3, 4, 5, 0.5)
     assert (call.logits, call.ld, call.ids, call.logp, call.entropy, call.top_ids, call.top_logp, call.d_err,
             call.workspace, call.workspace_bytes) == tuple(range(6, 16))
+    members = list(range(1, 7)) + [0.5] + list(range(7, 17))
+    call = tq.TqKvAttn.from_buffer_copy(tq._ATTN_CALL.pack(*members))
+    assert (call.n_rows, call.n_tokens, call.max_q, call.n_heads, call.max_len, call.window, call.scale, call.flags) == (
+        1, 2, 3, 4, 5, 6, 0.5, 7)
+    assert (call.seqs, call.cu_q, call.q.data, call.q.token_stride, call.q.head_stride, call.o, call.lse, call.workspace,
+            call.workspace_bytes) == tuple(range(8, 17))
+    call = tq.TqKvScope.from_buffer_copy(tq._SCOPE_CALL.pack(*range(1, 7)))
+    assert (call.sinks, call.n_groups, call.max_prefix, call.max_tail, call.cu_rows, call.prefix) == tuple(range(1, 7))
 
 
 def test_binding_refuses_what_is_not_on_the_gpu():

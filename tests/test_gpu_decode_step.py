@@ -150,6 +150,19 @@ def test_two_captured_steps_give_what_the_calls_give():
         assert torch.equal(a, b)
 
 
+def test_scales_that_32_bits_do_not_hold_are_refused():
+    s = Step(6)
+    s.fill(1)
+    q = s.parts(0)[0]
+    for scale in (1e39, -1e39, float("inf"), float("nan")):
+        for call in (lambda: tq.tq_rope(q, None, s.pos[0].zero_(), s.freq, scale=scale),
+                     lambda: tq.tq_logprobs(s.freq.view(1, 64), top=1, scale=scale),
+                     lambda: tq.tq_kv_attention(s.m.cache, 0, q, seqs=s.seqs, scale=scale),
+                     lambda: tq.tq_kv_attention(s.m.cache, 0, q, seqs=s.seqs, scale=scale, window=9, sinks=1)):
+            with pytest.raises(tq.TqError):
+                call()
+
+
 def test_tensors_of_another_device_are_refused(monkeypatch):
     s = Step(5)
     s.fill(1)
