@@ -254,16 +254,14 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
   Vec<T> next[NV];
   load(next, c0);
   for (int chunk = c0; chunk < c1; ++chunk) {
-    Vec<T> w[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) w[i] = next[i];
-    if (chunk + 1 < c1) load(next, chunk + 1);
     float v[kEach], most = none;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      v[e] = (float)w[e / VE].v[e % VE];
+      v[e] = (float)next[e / VE].v[e % VE];
+      asm("" : "+v"(v[e]));   // now, so that the next chunk's loads need no registers of their own
       most = fmaxf(most, v[e]);
     }
+    if (chunk + 1 < c1) load(next, chunk + 1);
     {
       const Ref r(fmaxf(z.m, most), c);
       if (most > z.m) {
