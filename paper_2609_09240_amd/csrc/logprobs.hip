@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
         ties += __builtin_amdgcn_readlane(incl, 63);
       }
       held += min(ties, k);
-      if (first && c1 > c0 + 1) {   // the bound of the whole chunk
+      if (first && c1 > c0 + 1 && k > 1) {   // the bound of the whole chunk (for one token it is there)
         rank_lists();
         held = wave == 0 ? k : 0;
         if (tid < k) list[0][tid] = best[tid];
