@@ -19,8 +19,8 @@
 //
 // What bounds it (8 heads of 128, groups of 64): 64 rows x 4 heads over 32768
 // shared tokens 111 us, of which vector instructions, 391 a record and tile, are 85
-// and matrix instructions 21; 16 rows over 8000 17.4: eight records a wave behind a
-// chain of loads.  The join 4 to 7.
+// and matrix instructions 21; 16 rows over 8000 18: eight records a wave behind a
+// chain of loads.  The join 4 to 6.
 
 #include "decode_internal.h"
 #include "kvattn_kernel.h"

@@ -16,9 +16,9 @@
 // workgroup of a row to leave its part joins them in their order.
 //
 // Bound by memory where rows are many and long: 1500 rows of 49999 fp16 logits
-// (150 MB) with the most likely one 47.6 us, 3.2 TB/s, of which vector instructions
-// are 32; without 39.  Few rows: 64 of 131072 fp32 logits (34 MB) 21 us with the 20
-// most likely ones, 13 without; 1 row of 5000 6.7: launch, two trips to memory,
+// (150 MB) with the most likely one 44.0 us, 3.4 TB/s, of which vector instructions
+// are 28; without 38.  Few rows: 64 of 131072 fp32 logits (34 MB) 21 us with the 20
+// most likely ones, 13 without; 1 row of 5000 6.6: launch, two trips to memory,
 // ranking, the join.
 
 #include "decode_internal.h"
@@ -64,7 +64,7 @@ __device__ inline float logit_of(uint64_t key) {
 // A logit relative to a reference, in powers of two.  (x - m) c and not x c - m c:
 // where scales are large or logits far from 0 what m c loses when it is rounded
 // would be more than there is between them.  (For 1500 rows of 49999 fp16 logits,
-// where x - m is almost always exact, it costs 1 to 2.7 us of 46.)
+// where x - m is almost always exact, it cost 1 to 2.7 us of 46.)
 struct Ref {
   float c, m;
   __device__ Ref(float m, float c) : c(c), m(fmaxf(m, kLowest)) {}
