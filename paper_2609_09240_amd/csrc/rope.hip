@@ -3,14 +3,16 @@
 //     (x1, x2) -> scale (x1 cos a - x2 sin a, x2 cos a + x1 sin a).
 //
 // Bound by memory: every channel is read and written once (8191 tokens of 32 + 8
-// heads of 128, 168 MB: 35 us, 4.8 TB/s).  A thread takes V pairs of one token for
+// heads of 128, 168 MB: 34.5 us, 4.9 TB/s).  A thread takes V pairs of one token for
 // several heads, so that its V angles are formed once for them: formed for every
 // two heads they take 55 us.  Four heads are loaded at a time, 8 or 10 are no
-// faster.  Stores past the caches take 33 instead of 43 us where inputs come from HBM,
-// and what reads the outputs next then takes longer by more than that: 72 instead of
-// 68 us for both, at 1024 tokens 15.0 instead of 14.3.  An angle is a product in 64 bits, reduced to a fraction of a turn there
+// faster.  An angle is a product in 64 bits, reduced to a fraction of a turn there
 // (what a position of 10^6 leaves of a product in 32 bits is 0.06), then sine and
 // cosine in 32 bits.
+//
+// Stores past the caches take 33 instead of 43 us where inputs come from HBM, but
+// what reads the outputs next then takes longer by more than that: 72 instead of
+// 68 us for both, at 1024 tokens 15.0 instead of 14.3.
 
 #include "decode_internal.h"
 
@@ -135,11 +137,12 @@ hipError_t launch_rope(const tq_rope_call& c, hipStream_t s) {
   a.turning = a.half / V;
   a.units = a.turning + rest / V;
   a.tokens = a.units <= 256 ? 256 / a.units : 1;
-  // Heads of a workgroup: four where there are few tokens, as many as leave two
-  // workgroups a CU, up to 20, where there are many (32 + 8 heads of 128: one
-  // token 5.2 us, with 20 heads a workgroup 9.2; 8191 tokens 35 us, with 4 41).
+  // Heads of a workgroup: four where there are few tokens, eight where fours would
+  // make more than 2.5 workgroups a CU (32 + 8 heads of 128 from HBM, with 4, 8, 20
+  // heads: 256 tokens 5.7, 7.2, 11.5 us; 2048: 14.7, 14.6, 19.2; 8191: 43.7, 40.4,
+  // 44.1, from caches 41, 35, 35).
   const int64_t fours = (int64_t)((a.n_tokens + a.tokens - 1) / a.tokens) * ((a.heads + 3) / 4);
-  a.per = 4 * (int)(fours < 1024 ? 1 : fours < 2560 ? fours / 512 : 5);
+  a.per = fours < 640 ? 4 : 8;
   const bool adjacent = c.flags & TQ_ROPE_ADJACENT;
   if (V == 8) return start<8, 4>(a, adjacent, s);
   if (V == 4) return start<4, 4>(a, adjacent, s);
