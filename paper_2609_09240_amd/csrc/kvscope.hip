@@ -18,7 +18,7 @@
 // tokens, and as long with its additional launch at 64 rows x 32768.)
 //
 // What bounds it (8 heads of 128, groups of 64): 64 rows x 4 heads over 32768
-// shared tokens 111 us, of which vector instructions, 391 a record and tile, are 85
+// shared tokens 108 us, of which vector instructions, 391 a record and tile, are 85
 // and matrix instructions 21; 16 rows over 8000 18: eight records a wave behind a
 // chain of loads.  The join 4 to 6.
 
@@ -44,7 +44,7 @@ struct Work {
 // What a launch of workgroups of `waves` waves takes (us), where `a` and `b` are cut
 // into parts.  A CU has its share of the workgroups of `a`, a whole number, and of
 // those of `b`.  A record takes a wave alone on its SIMD 1, two waves 1.6 and three 2.3;
-// 2.5 start and end a round of workgroups, 0.12 joins a part.  (64 rows of 4 heads over
+// 2.5 start and end a round of workgroups of four waves, 3.5 of eight; 0.12 joins a part.  (64 rows of 4 heads over
 // 32768 shared tokens, of which 128 tiles and heads are cut into 1, 2, 3, 4, 6, 8 parts:
 // 264, 140, 150, 117, 113, 113 us; 16 rows over 8000, 32 of them into 5, 6, 7, 8, 10, 12,
 // 15, 18: 24.8, 22.9, 21.1, 20.3, 23.6, 22.2, 20.9, 22.8.)
@@ -55,9 +55,9 @@ double cost(const KvDev& c, int waves, Work a, int parts_a, Work b, int parts_b)
   const double recs_a = a.ids > 0 ? (double)((a.recs + parts_a * waves - 1) / (parts_a * waves)) : 0.0;
   const double recs_b = b.ids > 0 ? (double)((b.recs + parts_b * waves - 1) / (parts_b * waves)) : 0.0;
   const double longest = recs_a > recs_b ? recs_a : recs_b;
-  const double of_simd = waves / 4.0 * ((double)((n_a + kCus - 1) / kCus) * recs_a + (double)n_b / kCus * recs_b);
+  const double of_simd = (double)((n_a + kCus - 1) / kCus) * a.recs / (4.0 * parts_a) + (double)b.ids * b.recs / (4.0 * kCus);
   const double busy = 0.73 * of_simd + 0.13 * longest;
-  return 2.5 * rounds + (busy > longest ? busy : longest) + 0.12 * (parts_a + parts_b);
+  return (waves == 8 ? 3.5 : 2.5) * rounds + (busy > longest ? busy : longest) + 0.12 * (parts_a + parts_b);
 }
 
 // The best parts of `a` beside `b`, in workgroups of `waves` waves; `join`: what
