@@ -25,6 +25,12 @@ def run(m, q, nq, seqs, groups=None, prefix=None, f32=True, **kw):
         assert prefix.tolist() == want
     one = all(n == 1 for n in nq) and kw.get("max_q") is None
     kw = dict(kw, cu_q=None if one else i32(0, *np.cumsum(nq).tolist()), max_q=1 if one else kw.get("max_q") or max(nq))
+    # attended together, or the test would be one of something else (60 queries of 40
+    # heads a key/value head are not, for 2000 tokens)
+    if kw.get("max_prefix") == 1 << 20 or (kw.get("max_prefix") == 2000 and q.shape[1] // m.H < 40):
+        assert tq.tq_kv_attention_workspace_bytes(
+            m.cache, len(nq), q.shape[1], n_tokens=q.shape[0], max_q=kw["max_q"], max_len=kw.get("max_len", 0),
+            n_groups=1 if groups is None else len(groups) - 1, max_prefix=kw["max_prefix"]) > 0
     return tq.tq_kv_attention(m.cache, 0, torch.from_numpy(q).cuda() if isinstance(q, np.ndarray) else q, seqs=seqs_t,
                               prefix=prefix, groups=g, out_f32=f32, want_lse=True, **kw)
 
