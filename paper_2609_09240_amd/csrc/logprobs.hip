@@ -1,7 +1,7 @@
 // Log probabilities of rows of logits (gfx950), one pass over them.  With t_j =
 // scale log2(e) (x_j - m), where m is the largest of them,
 //     S = sum 2^t_j,  T = sum 2^t_j t_j,
-//     log p_j = scale (x_j - m) - ln 2 log2 S,   H = ln 2 (log2 S - T / S);
+//     log p_j = scale (x_j - m) - log S,   H = log S - ln 2 T / S;
 // m moves, and the sums with it, whenever a thread's maximum grows.
 //
 // The most likely tokens.  A wave holds 1024 logits in registers.  The k-th
@@ -16,9 +16,9 @@
 // workgroup of a row to leave its part joins them in their order.
 //
 // Bound by memory where rows are many and long: 1500 rows of 49999 fp16 logits
-// (150 MB) with the most likely one 44.0 us, 3.4 TB/s, of which vector instructions
-// are 28; without 38.  Few rows: 64 of 131072 fp32 logits (34 MB) 21 us with the 20
-// most likely ones, 13 without; 1 row of 5000 6.6: launch, two trips to memory,
+// (150 MB) with the most likely one 47 us, 3.2 TB/s, of which vector instructions
+// are about 30; without 40.  Few rows: 64 of 131072 fp32 logits (34 MB) 22 us with the
+// 20 most likely ones, 13.6 without; 1 row of 5000 7.1: launch, two trips to memory,
 // ranking, the join.
 
 #include "decode_internal.h"
@@ -72,16 +72,18 @@ struct Ref {
   __device__ float from(const Ref& o) const { return (o.m - m) * c; }   // of o's reference
 };
 
-// Largest logit m, S and T against it.
+// Largest logit m, S - 1 and T against it: one of the logits that equal m is left
+// out of the sum, whose term is 1: the log probability of a token that is nearly
+// certain is that of the others' sum, which the steps of a sum near 1 would drown.
 struct Sums {
   float m, s, t;
+  __device__ float all() const { return (m > -__builtin_inff() ? 1.0f : 0.0f) + s; }
 };
 __device__ inline Sums join(Sums a, Sums b, float c) {
-  const Ref ra(a.m, c), rb(b.m, c), r(fmaxf(a.m, b.m), c);
-  const float da = fmaxf(r.from(ra), kLowest), db = fmaxf(r.from(rb), kLowest);
-  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-  const float sa = a.s * fa, sb = b.s * fb;
-  return Sums{fmaxf(a.m, b.m), sa + sb, fmaf(sa, da, a.t * fa) + fmaf(sb, db, b.t * fb)};
+  const bool first = a.m >= b.m;
+  const Sums w = first ? a : b, l = first ? b : a;
+  const float by = fmaxf(Ref(w.m, c).from(Ref(l.m, c)), kLowest), f = __builtin_amdgcn_exp2f(by), s = l.all() * f;
+  return Sums{w.m, w.s + s, w.t + fmaf(s, by, l.t * f)};
 }
 
 __device__ inline int below(uint64_t mask) {   // lanes of a mask before this one
@@ -264,18 +266,23 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
     if (chunk + 1 < c1) load(next, chunk + 1);
     {
       const Ref r(fmaxf(z.m, most), c);
-      if (most > z.m) {
+      // (The largest one's 1 is taken off where it comes: what is added after it is
+      // added to a small number.)
+      const bool grows = most > z.m;
+      float sum = grows ? -1.0f : 0.0f;
+      if (grows) {
         const float by = fmaxf(r.from(Ref(z.m, c)), kLowest), f = __builtin_amdgcn_exp2f(by);
-        z.s *= f;
+        z.s = z.all() * f;
         if (ENTROPY) z.t = fmaf(z.s, by, z.t * f);
         z.m = most;
       }
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
         const float t = r(v[e]), p = __builtin_amdgcn_exp2f(t);
-        z.s += p;
+        sum += p;
         if (ENTROPY) z.t = fmaf(p, fmaxf(t, kLowest), z.t);   // 0 times -infinity
       }
+      z.s += sum;
     }
     if constexpr (TOP) {
       const bool first = chunk == c0;
@@ -407,8 +414,8 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
   }
 
   // What is asked for.  Where no token is possible S is 0.
-  const bool empty = z.s == 0.0f;
-  const float log2_s = log2f(z.s), log_s = log2_s * kLn2;
+  const bool empty = z.all() == 0.0f;
+  const float log_s = log1pf(z.s);
   auto logp = [&](float v) { return empty ? none : (v - z.m) * a.scale - log_s; };
   for (int i = tid; i < a.n_ids; i += kThreads) {
     const int64_t at = (int64_t)row * a.n_ids + i;
@@ -417,7 +424,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
     a.logp[at] = in ? logp((float)x[id]) : __builtin_nanf("");
     if (!in && a.d_err != nullptr) atomicAdd(a.d_err, 1);
   }
-  if (ENTROPY && tid == 0) a.entropy[row] = empty ? 0.0f : (log2_s - z.t / z.s) * kLn2;
+  if (ENTROPY && tid == 0) a.entropy[row] = empty ? 0.0f : log_s - z.t / z.all() * kLn2;
   if constexpr (TOP) {
     if (tid < k) {
       const uint64_t key = best[tid];

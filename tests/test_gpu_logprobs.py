@@ -114,6 +114,25 @@ def test_small_and_large_scales(f32, scale):
 
 
 @pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("V", [2, 300, 5000, 49999, 131072])
+def test_a_token_that_is_nearly_certain(f32, V):
+    """Of the others' sum, exponentials (2 |z| + 4), the sums of a thread, of lanes,
+    waves and parts (V/256 + 64 + 12) and the logarithm (4) are off by u each; up to 16
+    terms are added to -1 before the token's own 1, in steps of u / 2."""
+    x = logits(6, V, 9, f32, 0.0, 1.0)
+    at = np.array([0, V - 1, V // 2, V // 3, 1, V // 7])
+    lead = np.log(V) + np.array([2.0, 4.0, 6.0, 9.0, 12.0, 15.0])
+    x[np.arange(6), at] = x.max(-1) + lead
+    got = run(x, at[:, None], top=1)
+    check(x, got, at[:, None], 1)
+    want = decode.logprobs(x, at[:, None], 1)[0][:, 0]
+    z = (x.max(-1) - x.min(-1)).astype(np.float64)
+    assert (want > -0.3).all() and (want < 0).all()
+    for lp in (got[0][:, 0], got[3][:, 0]):
+        assert (np.abs(lp.cpu().numpy() - want) <= (8 - want * (2 * z + 84 + V / 256)) * U).all()
+
+
+@pytest.mark.parametrize("f32", [False, True])
 def test_nothing_possible_and_special_values(f32):
     x = logits(9, 9000, 4, f32)
     low = np.finfo(x.dtype).min
