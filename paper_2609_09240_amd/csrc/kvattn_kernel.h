@@ -276,8 +276,10 @@ __device__ inline bool stack_of(const MoreArgs& a, int j, Tile* t) {
   return true;
 }
 
-// The last position that token `at` of the call sees of a group's shared tokens,
-// -1 where it sees none.
+// The last position that token `at` of the call sees of a group's shared tokens:
+// -1 where it sees none of them (its row asks for more queries than it holds
+// tokens), kNobody where kv_join_kernel does not take up what its tile gives.
+constexpr int kNobody = -2;
 __device__ inline int stack_pos(const MoreArgs& a, int b, int b1, int at) {
   int row = at;
   int64_t first = at, asked = 1;
@@ -295,8 +297,9 @@ __device__ inline int stack_pos(const MoreArgs& a, int b, int b1, int at) {
     asked = (int64_t)a.cu[row + 1] - first;
   }
   const int64_t i = at - first;
-  if (i < 0 || i >= asked || i >= a.max_q) return -1;
+  if (i < 0 || i >= asked || i >= a.max_q) return kNobody;
   const int len = length_of(a, a.seqs ? a.seqs[row] : row), shared = shared_of(a, row);
+  if (shared == 0) return kNobody;
   return (int)max(min((int64_t)shared, len - asked + i + 1), (int64_t)0) - 1;
 }
 
@@ -634,8 +637,8 @@ kv_attn_kernel(typename ArgsFor<MODE>::type args) {
     all1 = (int)max((int64_t)0, min((int64_t)t.len, base + t.tok0 + 1));
     if (a.window > 0) all0 = (int)max((int64_t)0, base + last + 1 - a.window);
     if constexpr (MODE == kShared)
-      if (stacked) {   // tokens that the call leaves out see nothing; nobody takes up what they get
-        all1 = in && pos >= 0 ? pos + 1 : INT32_MAX;
+      if (stacked) {   // one that sees no token has all of them masked
+        all1 = in && pos != kNobody ? pos + 1 : INT32_MAX;
 #pragma unroll
         for (int k = 1; k < 16; k *= 2) all1 = min(all1, __shfl_xor(all1, k));
       }

@@ -126,6 +126,30 @@ def test_a_query_inside_the_prefix_sees_its_past_only():
             check(m, q[:n], nq, o, lse, seqs=m.kids)
 
 
+@pytest.mark.parametrize("D,G,H,share,prompt,tails,nq", [
+    (64, 32, 1, 1, 64, [36, 0], [1, 80]),                   # 16 queries before the first token, beside one that sees all
+    (128, 64, 2, 4, 64, [36, 0], [1, 65]),                  # one of them among rows that see tokens
+    (64, 64, 1, 2, 40, [0, 0], [50, 50]),                   # tiles of nothing else
+    (256, 64, 1, 3, 100, [0, 5, 900, 1], [140, 1, 2, 103]),
+    (128, 128, 2, 1, 320, [1, 1, 1], [1, 322, 400]),
+])
+def test_queries_before_a_slots_first_token(D, G, H, share, prompt, tails, nq):
+    """Rows with more queries than their slots hold tokens: the first of them see
+    nothing, whatever the rows beside them in a tile see."""
+    m = Branches([prompt], [0] * len(tails), tails, H, D, G, 32, seed=D + share)
+    q = rows((sum(nq), H * share, D), 4)
+    for hint in (FEW, MANY, {}):
+        o, lse = run(m, q, nq, m.kids, **hint)
+        check(m, q, nq, o, lse, seqs=m.kids)
+    # those past max_q are left alone beside them (few queries of many tokens may be attended row by row)
+    for most, hint in ((3, dict(max_prefix=1 << 19)), (max(nq) - 1, MANY)):
+        o2 = torch.full_like(o, 9.0)
+        o2, lse2 = run(m, q, nq, m.kids, max_q=most, o=o2, **hint)
+        check(m, q, nq, o2, lse2, seqs=m.kids, max_q=most)
+        past = np.concatenate([np.arange(n) >= most for n in nq])
+        assert bool((o2.cpu()[past] == 9).all())
+
+
 def test_positions_without_a_page_and_poison():
     """A page that the table lost is left out; NaN and infinities in pages that
     nobody names, and behind the rows, do not show; those that are seen do."""
