@@ -332,7 +332,7 @@ __device__ inline bool tile_of(const A& a, int b, int qt, Tile* t) {
   t->rec1 = hi > lo ? (int)((hi + 31) >> 5) : t->rec0;
   if constexpr (MODE == kSinks) {
     t->win0 = t->rec0;
-    if (hi > lo) t->rec0 -= min(t->win0, (a.sinks + 31) >> 5);
+    if (hi > lo) t->rec0 -= min(t->win0, (min(a.sinks, t->len) + 31) >> 5);   // (a length leaves room for 31 more)
   }
   t->units = max(1, (t->rec1 - t->rec0 + kWaves - 1) / kWaves);
   return true;

@@ -80,6 +80,18 @@ def test_sinks_that_change_nothing():
     check(m, q, [1, 1], o, lse)
 
 
+@pytest.mark.parametrize("sinks", [2 ** 31 - 1, 2 ** 31 - 30, 2 ** 31 - 31, 2 ** 31 - 32, 2 ** 31 - 33])
+@pytest.mark.parametrize("nq", [[1, 1, 1], [3, 40, 1]])
+def test_as_many_sinks_as_there_are_numbers(sinks, nq):
+    """Every token, then: as if there were no window, in one part and in several."""
+    m = Model([5000, 70, 1], 2, 128, 64, 64, seed=3)
+    q = rows((sum(nq), 8, 128), 6)
+    for window in (1, 40, 2 ** 31 - 1):
+        for hint in (0, 100):
+            o, lse = run(m, q, nq, window=window, sinks=sinks, max_len=hint)
+            check(m, q, nq, o, lse)
+
+
 def test_what_may_not_be_seen_does_not_show():
     """NaN and infinite keys and values between the sinks and the window."""
     m = Model([200], 1, 64, 32, 32)
