@@ -2,7 +2,7 @@
 // scale log2(e) (x_j - m), where m is the largest of them,
 //     S = sum 2^t_j,  T = sum 2^t_j t_j,
 //     log p_j = scale (x_j - m) - log S,   H = log S - ln 2 T / S;
-// m moves, and the sums with it, whenever a thread's maximum grows.
+// m moves, and the sums with it, whenever a wave's maximum grows.
 //
 // The most likely tokens.  A wave holds 1024 logits in registers.  The k-th
 // largest of its 64 lanes' maxima bounds the k-th largest logit from below, and
@@ -74,7 +74,8 @@ struct Ref {
 
 // Largest logit m, S - 1 and T against it: one of the logits that equal m is left
 // out of the sum, whose term is 1: the log probability of a token that is nearly
-// certain is that of the others' sum, which the steps of a sum near 1 would drown.
+// certain is that of the others' sum, which the steps of a sum near 1 would drown,
+// wherever those others lie.
 struct Sums {
   float m, s, t;
   __device__ float all() const { return (m > -__builtin_inff() ? 1.0f : 0.0f) + s; }
@@ -140,10 +141,24 @@ __device__ inline float kth_of(float x, int k) {
   return lane_of(x, k - 1);
 }
 
+// The largest of the lanes' x, uniform.
+template <int CTRL>
+__device__ inline float max_dpp(float x) {
+  const int b = __builtin_bit_cast(int, x);
+  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CTRL, 0xF, 0xF, true)));
+}
 __device__ inline float wave_max(float x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
+  x = max_dpp<0xB1>(x);    // quad_perm 1 0 3 2
+  x = max_dpp<0x4E>(x);    // quad_perm 2 3 0 1
+  x = max_dpp<0x141>(x);   // row_half_mirror
+  x = max_dpp<0x140>(x);   // row_mirror
+  uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  uint32_t r0 = r[0], r1 = r[1];
+  b = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1)));
+  const auto w = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  r0 = w[0], r1 = w[1];
+  return lane_of(fmaxf(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1)), 0);
 }
 
 // Keys of a list of n, filled up with zeros to a multiple of 8, above one.
@@ -192,13 +207,16 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
   __shared__ float bounds[kWaves];
   __shared__ int counts[kWaves + 1];
   __shared__ int last;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
   const T* x = static_cast<const T*>(a.x) + row * a.ld;
-  const float c = a.scale * 1.4426950408889634f;
+  const float c = lane_of(a.scale * 1.4426950408889634f, 0);   // (uniform: no vector register)
   const int k = TOP ? a.k : 0;
   const float none = -__builtin_inff();
+  // The lane's sums against the largest logit of its wave, which is left out of
+  // those of lane `holder`.
   Sums z = {none, 0.0f, 0.0f};
+  int holder = -1;
   uint64_t* mine = list[TOP ? wave : 0];
   int held = 0;
   float bound = none;
@@ -264,31 +282,40 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
       most = fmaxf(most, v[e]);
     }
     if (chunk + 1 < c1) load(next, chunk + 1);
-    {
-      const Ref r(fmaxf(z.m, most), c);
-      // (The largest one's 1 is taken off where it comes: what is added after it is
-      // added to a small number.)
-      const bool grows = most > z.m;
-      float sum = grows ? -1.0f : 0.0f;
-      if (grows) {
-        const float by = fmaxf(r.from(Ref(z.m, c)), kLowest), f = __builtin_amdgcn_exp2f(by);
-        z.s = z.all() * f;
-        if (ENTROPY) z.t = fmaf(z.s, by, z.t * f);
-        z.m = most;
-      }
+    // A sum of 16 terms, of which `leaves_out` says which is none of it.
+    auto add = [&](auto leaves_out) {
+      const Ref r(z.m, c);
+      float sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
         const float t = r(v[e]), p = __builtin_amdgcn_exp2f(t);
-        sum += p;
+        sum += leaves_out(v[e]) ? 0.0f : p;
         if (ENTROPY) z.t = fmaf(p, fmaxf(t, kLowest), z.t);   // 0 times -infinity
       }
       z.s += sum;
+    };
+    if (__builtin_amdgcn_ballot_w64(most > z.m) == 0) {
+      add([](float) { return false; });
+    } else {
+      const float now = wave_max(most), by = fmaxf(Ref(now, c).from(Ref(z.m, c)), kLowest), f = __builtin_amdgcn_exp2f(by);
+      z.s = (lane == holder ? z.s + 1.0f : z.s) * f;
+      if (ENTROPY) z.t = fmaf(z.s, by, z.t * f);
+      z.m = now;
+      // The first logit that equals it, of the first lane that has one.  (+infinity is
+      // left in: its term is NaN.)
+      holder = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(most == now)) - 1;
+      bool out = lane == holder && now < __builtin_inff();
+      add([&](float x) {
+        const bool it = out && x == now;
+        out = out && !it;
+        return it;
+      });
     }
     if constexpr (TOP) {
       const bool first = chunk == c0;
       bool equal = first;
       if (first) {
-        const float b = k == 1 ? wave_max(most) : kth_of(most, k);
+        const float b = k == 1 ? z.m : kth_of(most, k);
         if (lane == 0) bounds[wave] = b;
         __syncthreads();
         bound = fmaxf(fmaxf(bounds[0], bounds[1]), fmaxf(bounds[2], bounds[3]));
@@ -346,7 +373,10 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
 
   // The workgroup's sums and keys.
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) z = join(z, Sums{__shfl_xor(z.m, d), __shfl_xor(z.s, d), __shfl_xor(z.t, d)}, c);
+  for (int d = 1; d < 64; d *= 2) {
+    z.s += __shfl_xor(z.s, d);
+    if (ENTROPY) z.t += __shfl_xor(z.t, d);
+  }
   if (lane == 0) sums[wave] = z;
   if constexpr (TOP) rank_lists();
   __syncthreads();

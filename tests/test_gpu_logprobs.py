@@ -132,6 +132,82 @@ def test_a_token_that_is_nearly_certain(f32, V):
         assert (np.abs(lp.cpu().numpy() - want) <= (8 - want * (2 * z + 84 + V / 256)) * U).all()
 
 
+def certain(T, V, f32, lead, at, rest):
+    """Rows of `rest` with the largest logit at `at` and `lead` below it one at every
+    place of V in turn; and those places."""
+    places = [j for j in (0, 1, 3, 4, 7, 8, 9, 100, 255, 256, 1023, 1024, 2047, 2048, 2049, 4095, 4096, 4101, 12289, V // 2,
+                          V - 9, V - 2, V - 1) if 0 <= j < V and j != at]
+    x = np.full((len(places), V), rest, np.float32)
+    x[:, at] = 20.0
+    x[np.arange(len(places)), places] = 20.0 - lead
+    return (x if f32 else x.astype(np.float16)), places
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("V", [2, 9, 300, 5000, 49999, 131072])
+@pytest.mark.parametrize("rest", [-np.inf, -60.0])
+def test_the_others_of_a_certain_token(f32, V, rest):
+    """What is left of 1 is the others' sum, wherever they lie beside the certain token: in
+    its thread, before and behind it, in other lanes, waves, chunks and parts.
+
+    Relative to it alone, with u = 2^-24 and z up to 80: an argument of an exponential
+    is off by 3 u z (constant, difference, product), the exponential by 4 u and 2 u for
+    each of up to 8 rescalings, the sums by V/256 + 64 + 12 terms' u, the logarithm by 4
+    u; the entropy's second sum by 4 u more, for its factors."""
+    tol = (3 * 80 + 4 + 16 + V / 256 + 76 + 4 + 4) * U
+    for at in sorted({0, 1, 5, 15, 77, 2050, 4097, V // 3, V - 1}):
+        if at >= V:
+            continue
+        for lead in (2.0, 12.0, 18.5, 40.0, 79.0):
+            x, places = certain(1, V, f32, lead, at, rest)
+            if not places:
+                continue
+            ids = np.stack([np.full(len(places), at), places], 1)
+            logp, ent, tops, tlp = (t.cpu().numpy().astype(np.float64) for t in run(x, ids, top=2))
+            z = x.astype(np.float64) - 20.0
+            p = np.exp(z)
+            p[:, at] = 0.0
+            others = p.sum(-1)
+            log_s = np.log1p(others)
+            want = log_s + (p * np.where(p > 0, -z, 0)).sum(-1) / (1 + others)
+            assert (tops[:, 0] == at).all() and (logp[:, 0] == tlp[:, 0]).all()
+            assert (np.abs(logp[:, 0] + log_s) <= tol * log_s).all(), (at, lead)
+            assert (np.abs(ent - want) <= tol * want).all(), (at, lead)
+            assert (np.abs(logp[:, 1] + lead + log_s) <= tol * (lead + log_s)).all(), (at, lead)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_certain_tokens_one_after_the_other(f32):
+    """Every chunk's largest logit above the last one's, and what the old ones are then."""
+    V = 45000
+    for step in (3.0, 9.0, 17.5):
+        x = np.full((9, V), -np.inf, np.float32)
+        for i, at in enumerate(range(5, V, 4096)):
+            for r in range(9):
+                x[r, at + 3 * r] = i * step
+                x[r, at + (r * 517) % 4000 + 40] = i * step - 8.0
+        x = x if f32 else x.astype(np.float16)
+        z = np.sort(x.astype(np.float64), -1)[:, ::-1] - x.max(-1, keepdims=True)
+        others = np.exp(z[:, 1:]).sum(-1)
+        want = np.log1p(others)
+        got = tq.tq_logprobs(torch.from_numpy(x).cuda(), top=1)[3][:, 0].cpu().numpy().astype(np.float64)
+        # as above, with z up to 183; what lies past 87 below, and is lost, is less than 2^-24 of it
+        assert (np.abs(got + want) <= (3 * 183 + 105 + V / 256) * U * want).all(), step
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_infinities_and_nan_beside_a_certain_token(f32):
+    x = np.full((8, 9000), -40.0, np.float32)
+    x[:, 4] = 30.0
+    x[0, 3], x[1, 5], x[2, 5000], x[3, 0] = np.nan, np.nan, np.nan, np.inf
+    x[4, 4], x[5, 8999] = np.inf, np.inf
+    x[6, [3, 5]] = 30.0                                     # three alike
+    x[7, 8999] = 30.0
+    x = x if f32 else x.astype(np.float16)
+    got = run(x, np.tile([[4, 8999]], (8, 1)), top=3)
+    check(x, got, np.tile([[4, 8999]], (8, 1)), 3)
+
+
 @pytest.mark.parametrize("f32", [False, True])
 def test_nothing_possible_and_special_values(f32):
     x = logits(9, 9000, 4, f32)
