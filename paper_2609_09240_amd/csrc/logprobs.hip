@@ -61,15 +61,19 @@ __device__ inline float logit_of(uint64_t key) {
   return __builtin_bit_cast(float, o ^ (o & 0x80000000u ? 0x80000000u : 0xFFFFFFFFu));
 }
 
-// A logit relative to a reference, in powers of two.  (x - m) c and not x c - m c:
-// where scales are large or logits far from 0 what m c loses when it is rounded
-// would be more than there is between them.  (For 1500 rows of 49999 fp16 logits,
-// where x - m is almost always exact, it cost 1 to 2.7 us of 46.)
+// Half of x - m, which is finite where both are: 3e38 and -3e38 are 6e38 apart.
+__device__ inline float half_of(float x, float m) { return fmaf(0.5f, x, -0.5f * m); }
+
+// A logit relative to a reference, in powers of two; c2 is twice scale log2(e).
+// (x - m) c and not x c - m c: where scales are large or logits far from 0 what
+// m c loses when it is rounded would be more than there is between them.  (For 1500
+// rows of 49999 fp16 logits, where x - m is almost always exact, it cost 1 to 2.7 us
+// of 46.)
 struct Ref {
-  float c, m;
-  __device__ Ref(float m, float c) : c(c), m(fmaxf(m, kLowest)) {}
-  __device__ float operator()(float x) const { return (x - m) * c; }
-  __device__ float from(const Ref& o) const { return (o.m - m) * c; }   // of o's reference
+  float c2, m;
+  __device__ Ref(float m, float c2) : c2(c2), m(fmaxf(m, kLowest)) {}
+  __device__ float operator()(float x) const { return half_of(x, m) * c2; }
+  __device__ float from(const Ref& o) const { return half_of(o.m, m) * c2; }   // of o's reference
 };
 
 // Largest logit m, S - 1 and T against it: one of the logits that equal m is left
@@ -80,10 +84,10 @@ struct Sums {
   float m, s, t;
   __device__ float all() const { return (m > -__builtin_inff() ? 1.0f : 0.0f) + s; }
 };
-__device__ inline Sums join(Sums a, Sums b, float c) {
+__device__ inline Sums join(Sums a, Sums b, float c2) {
   const bool first = a.m >= b.m;
   const Sums w = first ? a : b, l = first ? b : a;
-  const float by = fmaxf(Ref(w.m, c).from(Ref(l.m, c)), kLowest), f = __builtin_amdgcn_exp2f(by), s = l.all() * f;
+  const float by = fmaxf(Ref(w.m, c2).from(Ref(l.m, c2)), kLowest), f = __builtin_amdgcn_exp2f(by), s = l.all() * f;
   return Sums{w.m, w.s + s, w.t + fmaf(s, by, l.t * f)};
 }
 
@@ -210,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
   const T* x = static_cast<const T*>(a.x) + row * a.ld;
-  const float c = lane_of(a.scale * 1.4426950408889634f, 0);   // (uniform: no vector register)
+  const float c2 = lane_of(a.scale * 2.8853900817779268f, 0);   // (uniform: no vector register)
   const int k = TOP ? a.k : 0;
   const float none = -__builtin_inff();
   // The lane's sums against the largest logit of its wave, which is left out of
@@ -284,7 +288,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
     if (chunk + 1 < c1) load(next, chunk + 1);
     // A sum of 16 terms, of which `leaves_out` says which is none of it.
     auto add = [&](auto leaves_out) {
-      const Ref r(z.m, c);
+      const Ref r(z.m, c2);
       float sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
@@ -297,7 +301,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
     if (__builtin_amdgcn_ballot_w64(most > z.m) == 0) {
       add([](float) { return false; });
     } else {
-      const float now = wave_max(most), by = fmaxf(Ref(now, c).from(Ref(z.m, c)), kLowest), f = __builtin_amdgcn_exp2f(by);
+      const float now = wave_max(most), by = fmaxf(Ref(now, c2).from(Ref(z.m, c2)), kLowest), f = __builtin_amdgcn_exp2f(by);
       z.s = (lane == holder ? z.s + 1.0f : z.s) * f;
       if (ENTROPY) z.t = fmaf(z.s, by, z.t * f);
       z.m = now;
@@ -382,7 +386,7 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
   __syncthreads();
   z = sums[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) z = join(z, sums[w], c);
+  for (int w = 1; w < kWaves; ++w) z = join(z, sums[w], c2);
 
   if (a.parts > 1) {
     const __amdgpu_buffer_rsrc_t parts_of =
@@ -440,13 +444,13 @@ __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6
     }
 #pragma unroll
     for (int d = 1; d < kMaxParts; d *= 2)
-      z = join(z, Sums{__shfl_xor(z.m, d), __shfl_xor(z.s, d), __shfl_xor(z.t, d)}, c);
+      z = join(z, Sums{__shfl_xor(z.m, d), __shfl_xor(z.s, d), __shfl_xor(z.t, d)}, c2);
   }
 
   // What is asked for.  Where no token is possible S is 0.
   const bool empty = z.all() == 0.0f;
   const float log_s = log1pf(z.s);
-  auto logp = [&](float v) { return empty ? none : (v - z.m) * a.scale - log_s; };
+  auto logp = [&](float v) { return empty ? none : 2.0f * (half_of(v, z.m) * a.scale) - log_s; };
   for (int i = tid; i < a.n_ids; i += kThreads) {
     const int64_t at = (int64_t)row * a.n_ids + i;
     const int id = a.ids[at];

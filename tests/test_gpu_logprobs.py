@@ -253,6 +253,19 @@ def test_large_and_close_logits():
     assert lp[0].tolist()[0] == 0.0 and lp[0].tolist()[1] == -np.inf and ids[0].tolist() == [0, 2, 1]
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -126, 2.0 ** -120, 0.1, 0.5])
+@pytest.mark.parametrize("V", [4, 9000])
+def test_logits_whose_difference_fp32_does_not_hold(scale, V):
+    """3e38 and -3e38: 6e38 apart, which a scale below 1 may bring back."""
+    x = np.full((4, V), -np.inf, np.float32)
+    x[0, [0, 1, 2]] = 3e38, -3e38, 1.0
+    x[1, [V - 1, 0, 1]] = 3e38, -3.4e38, 3e38
+    x[2, :2] = -3.4e38
+    x[3, [0, V - 1]] = -3.4e38, 3.4e38
+    ids = np.tile([[0, 1, V - 1]], (4, 1))
+    check(x, run(x, ids, top=3, scale=scale), ids, 3, scale)
+
+
 def test_strides_shapes_and_what_was_not_asked_for():
     x = logits(7, 1003, 7, False)
     buf = torch.full((7, 2051), float("nan"), dtype=torch.float16, device="cuda")
