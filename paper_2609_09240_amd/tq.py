@@ -301,9 +301,23 @@ def _check(status, where):
         raise TqError(status, where)
 
 
-def _cuda(t, dtype, name):
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor on the GPU")
+def _cuda(t, dtype, name, here=None):
+    """Checks a tensor on the GPU; on device `here`, the current one whose stream
+    the call goes to, where it is given."""
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()) or (here is not None and t.get_device() != here):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on the {_place(here)}")
+
+
+def _here(at):
+    """The current device, whose stream a call goes to; refuses buffers that are on
+    another one, or (-1) on none."""
+    if at < 0 or at != torch.cuda.current_device():
+        raise ValueError("the tensors must be on the current device")
+    return at
+
+
+def _place(here):
+    return "GPU" if here is None else "current device"
 
 
 # --------------------------------------------------------------------------
@@ -728,10 +742,10 @@ def tq_q4_unpack_fp16(mat, w=None, stream=None):
     return w
 
 
-def _out_buffer(t, shape, dtype, name):
+def _out_buffer(t, shape, dtype, name, here=None):
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}")
-    _cuda(t, dtype, name)
+    _cuda(t, dtype, name, here)
 
 
 def tq_q4_workspace_bytes(mat, B):
@@ -781,7 +795,7 @@ class KVCache:
     calls below.  One cache serves one stream at a time: calls on another
     one are the caller's to order."""
 
-    __slots__ = ("data", "pages", "lens", "refs", "n_kv_heads", "head_dim", "page_size", "group", "_ref", "_ws")
+    __slots__ = ("data", "pages", "lens", "refs", "n_kv_heads", "head_dim", "page_size", "group", "_ref", "_ws", "_at")
 
     def __init__(self, data, pages, lens, refs, n_kv_heads, head_dim, page_size=64, group=64):
         _cuda(data, torch.uint8, "data")
@@ -802,6 +816,8 @@ class KVCache:
         self.n_kv_heads, self.head_dim, self.page_size, self.group = n_kv_heads, head_dim, page_size, group
         self._ref = ref
         self._ws = _Workspaces(data.device)
+        at = {t.get_device() for t in self._buffers()}
+        self._at = at.pop() if len(at) == 1 else -1   # the device of all buffers
 
     @classmethod
     def empty(cls, n_layers, n_pages, n_seqs, max_pages, n_kv_heads, head_dim, page_size=64, group=64,
@@ -826,13 +842,13 @@ class KVCache:
         return self.data, self.pages, self.lens, self.refs
 
 
-def _i32(t, n, name):
-    """An int32 vector of n elements on the GPU, or None."""
+def _i32(t, n, name, here=None):
+    """An int32 vector of n elements on the GPU (device `here`), or None."""
     if t is None:
         return None
     if t.dim() != 1 or t.numel() != n:
         raise ValueError(f"{name} must have {n} elements")
-    _cuda(t, torch.int32, name)
+    _cuda(t, torch.int32, name, here)
     return t.data_ptr()
 
 
@@ -978,10 +994,11 @@ def _f32(x):
     return x if -3e38 < x < 3e38 else math.inf
 
 
-def _heads(t, shape, name):
-    """Address and strides of fp16 [T, heads, D] on the GPU, any strides but the last."""
-    if t.dtype is not torch.float16 or not t.is_cuda or t.shape != shape:
-        raise ValueError(f"{name} must be float16 {list(shape)} on the GPU")
+def _heads(t, shape, name, here=None):
+    """Address and strides of fp16 [T, heads, D] on the GPU (device `here`), any
+    strides but the last."""
+    if t.dtype is not torch.float16 or t.shape != shape or (not t.is_cuda if here is None else t.get_device() != here):
+        raise ValueError(f"{name} must be float16 {list(shape)} on the {_place(here)}")
     ts, hs, one = t.stride()
     if one != 1:
         raise ValueError(f"{name} must have adjacent channels")
@@ -1005,15 +1022,15 @@ def tq_kv_attention_workspace_bytes(cache, n_rows, n_heads, n_tokens=None, max_q
         cache._ref, a, _SCOPE_CALL.pack(sinks, n_groups, max_prefix, max_tail, some, some)))
 
 
-def _scope(n, sinks, prefix, groups, max_prefix, max_tail):
+def _scope(n, sinks, prefix, groups, max_prefix, max_tail, here):
     """tq_kv_scope of n rows, or None where nothing is asked for."""
     if prefix is None:
         if groups is not None:
             raise ValueError("groups share what prefix says")
         return _SCOPE_CALL.pack(sinks, 0, 0, 0, 0, 0) if sinks else None
     n_groups = 1 if groups is None else groups.numel() - 1
-    return _SCOPE_CALL.pack(sinks, n_groups, max_prefix, max_tail, _i32(groups, n_groups + 1, "groups") or 0,
-                            _i32(prefix, n, "prefix"))
+    return _SCOPE_CALL.pack(sinks, n_groups, max_prefix, max_tail, _i32(groups, n_groups + 1, "groups", here) or 0,
+                            _i32(prefix, n, "prefix", here))
 
 
 def tq_kv_shared_prefix(cache, groups=None, seqs=None, prefix=None, stream=None):
@@ -1023,11 +1040,11 @@ def tq_kv_shared_prefix(cache, groups=None, seqs=None, prefix=None, stream=None)
     of them without.  Once after the page table changed, for all layers."""
     n = _n_rows(cache, seqs, None)
     n_groups = 1 if groups is None else groups.numel() - 1
-    _here(cache.lens)
+    here = _here(cache._at)
     if prefix is None:
         prefix = torch.empty(n, dtype=torch.int32, device=cache.lens.device)
-    _check(lib().tq_kv_shared_prefix(cache._ref, _i32(seqs, n, "seqs"), _i32(groups, n_groups + 1, "groups"), n_groups, n,
-                                     _i32(prefix, n, "prefix"), _stream(stream)), "tq_kv_shared_prefix")
+    _check(lib().tq_kv_shared_prefix(cache._ref, _i32(seqs, n, "seqs", here), _i32(groups, n_groups + 1, "groups", here),
+                                     n_groups, n, _i32(prefix, n, "prefix", here), _stream(stream)), "tq_kv_shared_prefix")
     _used_on(stream, seqs, groups, prefix, *cache._buffers())
     return prefix
 
@@ -1057,23 +1074,23 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
         raise ValueError("without cu_q, q must have one token a row")
     max_q = _most(max_q, cu_q, T)
     _fits(layer | max_q | max_len | window | sinks | max_prefix | max_tail)
-    scope = None
+    scope = here = None
     if sinks or prefix is not None or groups is not None:
-        _here(q)
-        scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail)
-    qr = _heads(q, (T, n_heads, cache.head_dim), "q")
+        here = _here(cache._at)
+        scope = _scope(n, sinks, prefix, groups, max_prefix, max_tail, here)
+    qr = _heads(q, (T, n_heads, cache.head_dim), "q", here)
     if o is None:
         o = torch.empty((T, n_heads, D), dtype=torch.float32, device=q.device) if out_f32 else _new_like(q)
     else:
-        _out_buffer(o, (T, n_heads, D), torch.float32 if out_f32 else torch.float16, "o")
+        _out_buffer(o, (T, n_heads, D), torch.float32 if out_f32 else torch.float16, "o", here)
     if lse is None:
         if want_lse:
             lse = torch.empty((T, n_heads), dtype=torch.float32, device=q.device)
     else:
-        _out_buffer(lse, (T, n_heads), torch.float32, "lse")
+        _out_buffer(lse, (T, n_heads), torch.float32, "lse", here)
     members = [n, T, max_q, n_heads, max_len, window, D ** -0.5 if scale is None else _f32(scale),
-               OUT_FP32 if out_f32 else OUT_FP16, _i32(seqs, n, "seqs") or 0, _i32(cu_q, n + 1, "cu_q") or 0, *qr,
-               o.data_ptr(), 0 if lse is None else lse.data_ptr(), 0, 0]
+               OUT_FP32 if out_f32 else OUT_FP16, _i32(seqs, n, "seqs", here) or 0,
+               _i32(cu_q, n + 1, "cu_q", here) or 0, *qr, o.data_ptr(), 0 if lse is None else lse.data_ptr(), 0, 0]
     a = _ATTN_CALL.pack(*members)
     L = lib()
     if scope is None:
@@ -1084,7 +1101,7 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
         if workspace is None:
             workspace = cache._ws.get(need, stream)
         else:
-            _cuda(workspace, torch.uint8, "workspace")
+            _cuda(workspace, torch.uint8, "workspace", here)
         members[-2:] = workspace.data_ptr(), workspace.numel()
         a = _ATTN_CALL.pack(*members)
     if scope is None:
@@ -1099,13 +1116,6 @@ def tq_kv_attention(cache, layer, q, seqs=None, cu_q=None, max_q=None, max_len=0
 # --------------------------------------------------------------------------
 # Rotary positions and log probabilities.
 # --------------------------------------------------------------------------
-
-def _here(t):
-    """Refuses a tensor of another device than the current one, whose stream a
-    call goes to."""
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError("the tensors must be on the current device")
-
 
 def _new_like(t):
     """A new tensor of t's shape and type, its elements adjacent."""
@@ -1127,36 +1137,36 @@ def tq_rope(q, k, positions, freq, axis=None, adjacent=False, inverse=False, sca
     if len(shape) != 3:
         raise ValueError("q must be float16 [tokens, heads, D]")
     T, n_heads, D = shape
+    here = _here(q.get_device())
     at = positions.shape
-    if len(at) not in (1, 2) or at[-1] != T or positions.dtype is not torch.int32 or not positions.is_cuda or \
+    if len(at) not in (1, 2) or at[-1] != T or positions.dtype is not torch.int32 or positions.get_device() != here or \
             (T > 1 and positions.stride(-1) != 1):
-        raise ValueError("positions must be int32 [tokens] or [axes, tokens] on the GPU")
+        raise ValueError("positions must be int32 [tokens] or [axes, tokens] on the current device")
     axes = 1 if len(at) == 1 else at[0]
-    _cuda(freq, torch.float32, "freq")
+    _cuda(freq, torch.float32, "freq", here)
     n = freq.numel()
     if axis is not None:
-        _cuda(axis, torch.uint8, "axis")
+        _cuda(axis, torch.uint8, "axis", here)
         if axis.numel() != n:
             raise ValueError("axis must name one for every frequency")
     elif axes > 1:
         raise ValueError("several axes need axis")
-    qr = _heads(q, shape, "q")
+    qr = _heads(q, shape, "q", here)
     if q_out is None:
         q_out = _new_like(q)
         qo = (q_out.data_ptr(), n_heads * D, D)
     else:
-        qo = _heads(q_out, shape, "q_out")
+        qo = _heads(q_out, shape, "q_out", here)
     kr = ko = (0, 0, 0)
     kv_heads = 0
     if k is not None:
         kv_heads = k.shape[1] if k.dim() == 3 else 0
-        kr = _heads(k, (T, kv_heads, D), "k")
+        kr = _heads(k, (T, kv_heads, D), "k", here)
         if k_out is None:
             k_out = _new_like(k)
             ko = (k_out.data_ptr(), kv_heads * D, D)
         else:
-            ko = _heads(k_out, k.shape, "k_out")
-    _here(q)
+            ko = _heads(k_out, k.shape, "k_out", here)
     call = _ROPE_CALL.pack(T, n_heads, kv_heads, D, 2 * n, axes,
                            (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0), _f32(scale),
                            positions.data_ptr(), 0 if axes == 1 else positions.stride(0), freq.data_ptr(),
@@ -1194,11 +1204,11 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
     if one != 1 and V != 1:
         raise ValueError("logits must have adjacent elements in a row")
     _fits(T | V | top)
-    _here(logits)
+    here = _here(logits.get_device())
     logp = entropy = top_ids = top_logp = None
     m = 0
     if ids is not None:
-        _cuda(ids, torch.int32, "ids")
+        _cuda(ids, torch.int32, "ids", here)
         if ids.dim() not in (1, 2) or ids.shape[0] != T:
             raise ValueError("ids must be int32 [T] or [T, m]")
         m = 1 if ids.dim() == 1 else ids.shape[1]
@@ -1211,7 +1221,7 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
     members = [T, V, m, top, LOGITS_FP32 if logits.dtype is torch.float32 else LOGITS_FP16, _f32(scale),
                logits.data_ptr(), ld if T > 1 else V,
                *[0 if t is None else t.data_ptr() for t in (ids, logp, entropy, top_ids, top_logp)],
-               _i32(d_err, 1, "d_err") or 0, 0, 0]
+               _i32(d_err, 1, "d_err", here) or 0, 0, 0]
     L = lib()
     call = _LOGPROBS_CALL.pack(*members)
     need = L.tq_logprobs_workspace_bytes(call)
@@ -1222,7 +1232,7 @@ def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=No
                 ws = _logprobs_ws[logits.device] = _Workspaces(logits.device)
             workspace = ws.get(need, stream)
         else:
-            _cuda(workspace, torch.uint8, "workspace")
+            _cuda(workspace, torch.uint8, "workspace", here)
         members[-2:] = workspace.data_ptr(), workspace.numel()
         call = _LOGPROBS_CALL.pack(*members)
     _check(L.tq_logprobs(call, _stream(stream)), "tq_logprobs")
