@@ -61,10 +61,12 @@ double cost(const KvDev& c, int waves, Work a, int parts_a, Work b, int parts_b)
 }
 
 // The best parts of `a` beside `b`, in workgroups of `waves` waves; `join`: what
-// another launch that joins parts takes.  A part is a record a wave at least.
+// another launch that joins parts takes.  A part is a record a wave at least, and all
+// of them fit a grid, which holds fewer than 2^32 threads (1e30 where none do).
 double split(const KvDev& c, int waves, Work a, Work b, int parts_b, double join, int* parts) {
   double best = 1e30;
   for (int n = 1; n <= kMaxParts && (n == 1 || a.recs >= (int64_t)waves * n); n += n < 16 ? 1 : n / 8) {
+    if ((a.ids * n + b.ids * parts_b) * waves * 64 >= (int64_t)1 << 32) break;
     const double t = cost(c, waves, a, n, b, parts_b) + (n > 1 ? join : 0.0);
     if (t < best) {
       best = t;
@@ -78,7 +80,7 @@ bool plan(const KvDev& c, const AttnCall& a, const ScopeCall& sc, ScopePlan* p) 
   const int share = a.n_heads / c.H;
   const int64_t rows = (int64_t)a.max_q * share, tiles = (rows + 15) / 16, ids = tiles * a.n_rows * c.H;
   const int64_t hint = length_hint(c, a), part_bytes = (int64_t)a.n_tokens * a.n_heads * (c.D + 4) * 4;
-  // What a grid holds: with 256 threads a workgroup, and with 512 of two kinds.
+  // What a grid holds in one part: with 256 threads a workgroup, and with 512 of two kinds.
   constexpr int64_t kMostIds = 1 << 23, kMostOfTwo = 1 << 21;
   p->plain = p->sinks = false;
   p->stack_parts = p->stack_tiles = 0;
