@@ -200,7 +200,6 @@ struct Tile {
   int units;                 // of four records, one a wave; 1 where there are none
   int win0;                  // kSinks: records rec0 .. win0 - 1 stand for the first ones of the slot
   int b1;                    // stacked: the group's rows are b .. b1 - 1
-  int shared;                // kShared: tokens whose sums the group's tiles give
 };
 
 // x / share for x < share + 16 <= 2^16.
@@ -327,7 +326,7 @@ __device__ inline bool tile_of(const A& a, int b, int qt, Tile* t) {
   const int last = min(t->tok0 + by_share(a, t->head0 + 15), t->n - 1);
   const int64_t hi = min((int64_t)t->len, base + last + 1);
   int64_t lo = a.window > 0 ? max((int64_t)0, base + t->tok0 + 1 - a.window) : 0;
-  if constexpr (MODE == kShared) lo = t->shared = shared_of(a, b);
+  if constexpr (MODE == kShared) lo = shared_of(a, b);   // the group's tiles give the sums of those before
   t->rec0 = (int)(lo >> 5);
   t->rec1 = hi > lo ? (int)((hi + 31) >> 5) : t->rec0;
   if constexpr (MODE == kSinks) {
