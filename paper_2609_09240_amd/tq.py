@@ -304,7 +304,7 @@ def _check(status, where):
 def _cuda(t, dtype, name, here=None):
     """Checks a tensor on the GPU; on device `here`, the current one whose stream
     the call goes to, where it is given."""
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()) or (here is not None and t.get_device() != here):
+    if not ((t.is_cuda if here is None else t.get_device() == here) and t.dtype == dtype and t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor on the {_place(here)}")
 
 
