@@ -142,7 +142,8 @@ __device__ inline float log2_of(float x) { return (float)((int)(__builtin_bit_ca
 // (stacked: the queries of all of a group's rows as the rows of its tiles), and
 // rows over what is behind those.  (A chunk of 2 x 700 queries over up to 5000, 14
 // heads of 64 on 2, groups of 32, window 777 and 37 sinks: 32 us, 359 vector
-// instructions a record and tile, 61 % of the vector slots.)
+// instructions a record and tile, but 61 % of the vector slots: a wave has six or seven
+// records between a chain of loads at the start and a join of four waves.)
 enum { kPlain, kSinks, kShared };
 
 struct Args {
@@ -448,7 +449,8 @@ __device__ inline A args_anew() {
 
 // Waves a SIMD holds of a variant, as many as its vector registers allow without
 // a spill (512 / waves of them; past 256 half of them are accumulation registers
-// that cost moves).
+// that cost moves).  <256, 32> with sinks or shared tokens spills five for all that: 32
+// rows of 16 heads on 4 behind a window of 1024 37 us, 28 in groups of 64.
 constexpr int waves_of(int D, int G) { return D == 64 ? 4 : D == 128 ? (G == 32 ? 2 : 3) : 1; }
 
 template <int D, int G, int MODE, int W = kWaves>

@@ -4,8 +4,8 @@
 // Sinks: the records of a tile are those of its window and, in front of them,
 // the first ones of the slot; masks in the records where they end.  The host
 // decides the parts and the waves (8 of them to a tile where the chip is not full:
-// 32 rows of 8 heads behind a window of 1024 and 4 sinks 15.4 us, where the launch
-// for rows without sinks takes 23.6 behind the same window).
+// 32 rows of 8 heads behind a window of 1024 and 4 sinks 15.3 us; the launch that
+// rows without sinks still take needs 23.6 behind the same window).
 //
 // Shared prefixes.  The softmax over all tokens of a row is joined from those over
 // any parts of them: with m the largest logit of a part, l = sum exp(s - m) and
@@ -13,14 +13,17 @@
 //     o = sum_parts exp(m - M) y / sum_parts exp(m - M) l,   M = max of the m.
 // One launch takes the queries of all rows of a group as the rows of its tiles
 // over the shared records, and every row over what it has behind them; a second
-// one joins.  (Unpacking a record once into LDS for 128 or 256 stacked rows, as two
+// one joins.  A query of a row that asks for more of them than it holds tokens may see
+// none: its sums are 0 in every part then.  (Unpacking a record once into LDS for 128 or 256 stacked rows, as two
 // fp16 halves of every value, took 1.3 to 1.8 times as long up to 8192 shared
 // tokens, and as long with its additional launch at 64 rows x 32768.)
 //
 // What bounds it (8 heads of 128, groups of 64): 64 rows x 4 heads over 32768
 // shared tokens 108 us, of which vector instructions, 391 a record and tile, are 85
 // and matrix instructions 21; 16 rows over 8000 18: eight records a wave behind a
-// chain of loads.  The join 4 to 6.
+// chain of loads (16 heads of 256 on 4: 31 in groups of 64, 38 in groups of 32).  The
+// join 4 to 6.  tq_kv_shared_prefix, a workgroup a group that walks its rows: 16 rows
+// of 125 pages 6.4, 64 of 512 44, 512 of 32 in eight groups 20 and in one 113.
 
 #include "decode_internal.h"
 #include "kvattn_kernel.h"

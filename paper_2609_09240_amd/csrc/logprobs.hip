@@ -16,10 +16,11 @@
 // workgroup of a row to leave its part joins them in their order.
 //
 // Bound by memory where rows are many and long: 1500 rows of 49999 fp16 logits
-// (150 MB) with the most likely one 47 us, 3.2 TB/s, of which vector instructions
-// are about 30; without 40.  Few rows: 64 of 131072 fp32 logits (34 MB) 22 us with the
-// 20 most likely ones, 13.6 without; 1 row of 5000 7.1: launch, two trips to memory,
-// ranking, the join.
+// (150 MB) with the most likely one 46 us, 3.2 TB/s, of which vector instructions
+// are about 29; without 38.  Few rows: 64 of 131072 fp32 logits (34 MB) 21 us with the
+// 20 most likely ones, 13.4 without: a part has two chunks, between which the whole
+// workgroup ranks; one row of 131072 fp16 logits in 16 parts 14.  1 row of 5000 6.8:
+// launch, two chunks in one workgroup, ranking after either.
 
 #include "decode_internal.h"
 
@@ -202,6 +203,9 @@ struct __attribute__((packed, aligned(sizeof(T)))) Vec {
   T v[16 / sizeof(T)];
 };
 
+// Six waves a SIMD, 80 vector registers: fp16 with the entropy and the most likely
+// tokens spills three of them, and 30 to 42 scalar ones go to lanes of vector registers.
+// With five waves nothing is spilled and 1500 rows of 49999 take 60 us instead of 47.
 template <class T, bool ENTROPY, bool TOP>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) logprobs_kernel(LogArgs a) {
   constexpr int VE = 16 / sizeof(T), NV = kEach / VE;

@@ -2,8 +2,11 @@
 // token's position on the pair's axis,
 //     (x1, x2) -> scale (x1 cos a - x2 sin a, x2 cos a + x1 sin a).
 //
-// Bound by memory: every channel is read and written once (8191 tokens of 32 + 8
-// heads of 128, 168 MB: 34.5 us, 4.9 TB/s).  A thread takes V pairs of one token for
+// Bound by memory where there are many tokens: every channel is read and written once
+// (8191 tokens of 32 + 8 heads of 128, 168 MB: 35 us on three axes, 4.8 TB/s, 32 on
+// one).  Few tokens are bound by trips to memory one behind the other: of each of a
+// thread's eight pairs the axis, if it is given, and the position there, before any
+// channel is loaded (1 token 5.4 us, 5.8 on three axes; 64 tokens 5.5 and 5.9).  A thread takes V pairs of one token for
 // several heads, so that its V angles are formed once for them: formed for every
 // two heads they take 55 us.  Four heads are loaded at a time, 8 or 10 are no
 // faster.  An angle is a product in 64 bits, reduced to a fraction of a turn there
@@ -140,7 +143,7 @@ hipError_t launch_rope(const tq_rope_call& c, hipStream_t s) {
   // Heads of a workgroup: four where there are few tokens, eight where fours would
   // make more than 2.5 workgroups a CU (32 + 8 heads of 128 from HBM, with 4, 8, 20
   // heads: 256 tokens 5.7, 7.2, 11.5 us; 2048: 14.7, 14.6, 19.2; 8191: 43.7, 40.4,
-  // 44.1, from caches 41, 35, 35).
+  // 44.1, from caches 41, 35, 35; all of them on one axis, without an array of axes).
   const int64_t fours = (int64_t)((a.n_tokens + a.tokens - 1) / a.tokens) * ((a.heads + 3) / 4);
   a.per = fours < 640 ? 4 : 8;
   const bool adjacent = c.flags & TQ_ROPE_ADJACENT;

@@ -981,7 +981,8 @@ def tq_kv_read(cache, layer, starts, n_tokens, seqs=None, cu_new=None, max_new=N
 
 
 # tq_kv_attn, tq_kv_scope, tq_rope_call and tq_logprobs_call as bytes: building
-# a ctypes structure of as many members takes 2 us more.
+# a ctypes structure of as many members takes 2 us more.  (TqKvAttn and the others
+# name the members; tests hold the two against each other.)
 _ATTN_CALL = struct.Struct("@6ifiPPPqq3PN")
 _SCOPE_CALL = struct.Struct("@4iPP")
 _ROPE_CALL = struct.Struct("@7ifPqPP" + 4 * "Pqq")
@@ -1189,7 +1190,7 @@ def tq_logprobs_workspace_bytes(n_rows, n_vocab, n_ids=1, n_top=0):
 
 def tq_logprobs(logits, ids=None, top=0, scale=1.0, want_entropy=False, d_err=None, workspace=None, stream=None):
     """Log probabilities under softmax(scale * logits) of rows of logits
-    [T, V] (fp16 or fp32, any row stride): of given tokens ids (int32 [T] or
+    [T, V] (fp16 or fp32, any row stride from V on): of given tokens ids (int32 [T] or
     [T, m]), the entropy, and the `top` most likely tokens, the lower index
     first where logits are equal.  Returns (logp, entropy, top_ids, top_logp):
     fp32 of the shape of ids, fp32 [T], int32 and fp32 [T, top], None for what
