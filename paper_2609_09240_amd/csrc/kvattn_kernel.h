@@ -276,10 +276,11 @@ __device__ inline bool stack_of(const MoreArgs& a, int j, Tile* t) {
   return true;
 }
 
+constexpr int kNobody = -2;
+
 // The last position that token `at` of the call sees of a group's shared tokens:
 // -1 where it sees none of them (its row asks for more queries than it holds
 // tokens), kNobody where kv_join_kernel does not take up what its tile gives.
-constexpr int kNobody = -2;
 __device__ inline int stack_pos(const MoreArgs& a, int b, int b1, int at) {
   int row = at;
   int64_t first = at, asked = 1;
